@@ -1,5 +1,6 @@
 /*
  * gvc.h - C ABI of the Gated VLA-Cache control-step library for MI355X (gfx950).
+ * The control step comes first; the paged cache's operators are at the end.
  *
  * One control step of a Llama-2-shaped vision-language-action decoder in which
  * visually static image-patch tokens reuse the K/V they had at the previous
@@ -343,6 +344,113 @@ int32_t gvc_profile_end(gvc_ctx* ctx, double* total_ms, int32_t* launches);
 /* Frees the host context, after the work running on the GPU (its pinned memory
  * is freed).  Device memory stays with the caller. */
 int32_t gvc_destroy(gvc_ctx* ctx);
+
+/* ------------------------------------------------------------- paged cache
+ * Keys and values of many sequences in pages of one pool, for histories that
+ * outgrow a context's fixed prompt: rows are appended with their norm and
+ * rotation applied, and attend from one new token per sequence or from any
+ * list of rows.  These calls need no context; the caller owns the pages, the
+ * page table and the workspace, and gives the stream with each call.
+ *
+ * Slot j of sequence s is in page page_table[s][j / page_size] at j % page_size.
+ *   k_pages: dev [n_pages][n_kv_heads][page_size][head_dim]
+ *   v_pages: dev [n_pages][n_kv_heads][head_dim][page_size] (dim-major)
+ *   page_table: dev int32 [n_seqs][max_pages]
+ * Entries of pages that a call does not reach may hold anything.  An entry
+ * outside [0, n_pages) is no page: its slots are neither read nor written,
+ * and no row sees them.  A page may be in the lists of several sequences.
+ *
+ * A row sees slot j iff j <= its last slot and (window == 0 or j > last -
+ * window or j < n_sinks).  Its output is softmax(scale q.k) v over what it
+ * sees, zero where that is nothing; query head h reads key-value head
+ * h / (n_heads / n_kv_heads).  Slots that a row does not see do not reach its
+ * output, whatever they hold (NaN and infinities included).
+ *
+ * Rows: q, k, v and outputs are dev [rows][heads][head_dim] whose rows lie
+ * `stride` elements apart (heads dense), so a fused projection's rows can be
+ * given as they are; these pointers must be 16-byte aligned and the strides
+ * multiples of 8.  Scores, softmax statistics and norms are fp32.  Calls are
+ * asynchronous on `stream` (NULL = the null stream) of the current GPU, may
+ * be captured into a graph, and run on several streams at once if their
+ * workspaces, outputs and written slots are apart.  No call allocates device memory. */
+enum gvc_dtype { GVC_BF16 = 0, GVC_FP16 = 1 };
+
+typedef struct gvc_paged_desc {
+  int32_t dtype;          /* enum gvc_dtype: of q, k, v, norm gains, pages and outputs */
+  int32_t n_heads;        /* query heads, a multiple of n_kv_heads; at most 1024 */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t page_size;      /* slots of a page: 16, 32, 64 or 128 */
+  int32_t n_pages;        /* pages of the pool, >= 1 */
+  int32_t n_seqs;         /* rows of the page table, 1 to 4096 */
+  int32_t max_pages;      /* entries of a page-table row; max_pages * page_size <= 2^30 */
+} gvc_paged_desc;
+
+/* Norm and rotation of gvc_paged_append.  With gains, each head x of q (of k)
+ * becomes x / sqrt(mean x^2 + rms_eps) * gain first.  Then pair i < n = sum of
+ * pairs, of dimensions i and i + n, turns by position * theta^(-i/n), where
+ * the position is that of the pair's axis: the first pairs[0] pairs use axis
+ * 0, the next pairs[1] axis 1, the others axis 2 (time, height, width of a
+ * video patch, say).  Dimensions from 2 n on are not rotated. */
+typedef struct gvc_paged_rope {
+  int32_t pairs[3];       /* >= 0; their sum n a multiple of 4, 0 <= 2 n <= head_dim */
+  float theta;            /* > 0 */
+  float rms_eps;          /* >= 0 */
+  const void* q_norm;     /* dev [head_dim] or NULL */
+  const void* k_norm;     /* dev [head_dim] or NULL */
+  const int32_t* positions; /* dev int32 [3][position_stride], position_stride >= n_rows (axes
+                             whose pairs are 0 are not read), or NULL: every axis uses the row's slot */
+  int64_t position_stride;
+} gvc_paged_rope;
+
+/* Writes rows into the pages: k with norm and rotation, v as it is; q_out gets
+ * q with norm and rotation.  Row r belongs to slot row_slot[r] of sequence
+ * row_seq[r] (dev int32 [n_rows] each, in any order).  A row whose sequence,
+ * slot or page does not exist (a padding row: sequence -1) writes no slot; its
+ * q_out is written all the same.  Two rows of one call must not name the same
+ * slot (gvc_paged_check finds that), else either may be left there, element by
+ * element.  q and q_out may both be NULL (keys and values only).  q_out must
+ * not overlap the inputs.  n_rows * (n_heads + 2 n_kv_heads) < 2^28.  Errors:
+ * GVC_EINVAL, GVC_EDEVICE. */
+int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
+                         const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,
+                         const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream);
+
+/* Device bytes of workspace that gvc_paged_decode (n_rows = n_seqs) or
+ * gvc_paged_prefill with n_rows rows needs: partial results where the slots of
+ * a row are split over workgroups.  Errors: GVC_EINVAL. */
+int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, size_t* bytes);
+
+/* Attention of one token per sequence: row s of q sees the first lengths[s]
+ * slots of sequence s (dev int32 [n_seqs]; 0 or less: none, an idle slot of the
+ * batch) as far as the window goes.  q, out: dev [n_seqs][n_heads][head_dim].
+ * Errors: GVC_EINVAL, GVC_ENOMEM (short workspace), GVC_EDEVICE. */
+int32_t gvc_paged_decode(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                         int64_t q_stride, const int32_t* lengths, const void* k_pages, const void* v_pages,
+                         const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Attention of a list of rows: rows row_begin[s] to row_begin[s + 1] - 1 (dev
+ * int32 [n_seqs + 1], rising, at most n_rows) belong to sequence s, and row r's
+ * last slot is row_last[r] (dev int32 [n_rows]; -1: sees nothing).  Causal rows
+ * give their own slot, rows of a block that see each other both ways the
+ * block's last one; a sequence's rows may be any of its slots, and rising slots
+ * are fastest.  Rows outside every sequence's range are left as they were in out.  q, out:
+ * dev [n_rows][n_heads][head_dim]; n_rows * n_heads < 2^28.  Errors: GVC_EINVAL, GVC_ENOMEM (short workspace), GVC_EDEVICE. */
+int32_t gvc_paged_prefill(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                          int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows,
+                          const void* k_pages, const void* v_pages, const int32_t* page_table, void* out,
+                          int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Host-side check of what the calls above are given on the device: all
+ * pointers are host memory.  page_table int32 [n_seqs][max_pages]; lengths
+ * int32 [n_seqs] or NULL: the slots of each sequence that are to be read, whose pages must exist;
+ * row_seq, row_slot int32 [n_rows] (NULL with n_rows = 0): rows to be
+ * appended, whose sequence (or -1), slot and page must exist, no two in the
+ * same place of the pool.  GVC_OK, or GVC_EINVAL with the first fault in gvc_last_error. */
+int32_t gvc_paged_check(const gvc_paged_desc* desc, const int32_t* page_table, const int32_t* lengths,
+                        const int32_t* row_seq, const int32_t* row_slot, int32_t n_rows);
 
 /* Thread-local text of the last error ("" if none). */
 const char* gvc_last_error(void);

@@ -2,6 +2,7 @@
 // the per-call launch sequences of the C ABI declared in include/gvc.h.
 #include "gvc.h"
 #include "gvc_kernels.h"
+#include "gvc_paged.h"
 
 #include <algorithm>
 #include <cmath>
@@ -1436,3 +1437,12 @@ int32_t gvc_destroy(gvc_ctx* c) {
 }
 
 }  // extern "C"
+
+int32_t gvc::set_error(int32_t code, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {
+    g_err.clear();
+  }
+  return code;
+}

@@ -1,0 +1,113 @@
+// Internal declarations of the paged key-value cache's operators: what their
+// kernels take, their launchers, and the device code that they share.
+#pragma once
+#include "gvc.h"
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gvc {
+
+// Sets gvc_last_error and returns code (defined beside the error text).
+int32_t set_error(int32_t code, const char* msg) noexcept;
+
+// The pool as the kernels see it.  Offsets inside one page fit 32 bits (at
+// most 1024 heads x 128 slots x 128 dimensions); a page's own offset may not.
+struct PagedPool {
+  uint16_t* k;         // [n_pages][Hk][page][dh]
+  uint16_t* v;         // [n_pages][Hk][dh][page]
+  const int* table;    // [n_seqs][max_pages]
+  int n_seqs, max_pages, n_pages, page_shift;   // page = 1 << page_shift slots
+  int H, Hk, dh;
+};
+
+constexpr int kPagedMaxPairs = 64;   // head_dim / 2
+constexpr int kPagedMaxSeqs = 4096;  // their first tiles are kept in LDS
+
+struct PagedAppendArgs {
+  PagedPool pool;
+  const uint16_t *q, *kin, *vin, *q_norm, *k_norm;
+  uint16_t* q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const int *row_seq, *row_slot, *positions;   // positions: nullptr = the row's slot on every axis
+  int64_t position_stride;
+  int n_rows, n_pairs, end0, end1;             // pairs [0, end0) use axis 0, [end0, end1) axis 1, the others axis 2
+  float eps;
+  double turns[kPagedMaxPairs];                // pair i turns by position * turns[i] full turns
+};
+
+struct PagedAttnArgs {
+  PagedPool pool;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t q_stride, out_stride;
+  const int* row_last;    // last slot of each row; decode: the sequences' lengths
+  const int* row_begin;   // rows of each sequence, or nullptr: row s is sequence s, and row_last holds lengths
+  int n_rows, window, n_sinks;
+  float scale_log2e;      // scores in powers of two
+};
+
+hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, hipStream_t s);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, hipStream_t s);
+
+#ifdef __HIPCC__
+// ------------------------------------------------------------------ device
+typedef __bf16 pbf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 pf16x8 __attribute__((ext_vector_type(8)));
+typedef float pf32x4 __attribute__((ext_vector_type(4)));
+typedef float pf32x16 __attribute__((ext_vector_type(16)));
+typedef float pf32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t pu32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t pu32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t pu16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t pu16x8 __attribute__((ext_vector_type(8)));
+
+// The two 16-bit types.  Conversions to 16 bits round to nearest even.
+struct Bf16 {
+  typedef __bf16 elem;
+  typedef pbf16x8 x8;
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ float up(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
+  static __device__ __forceinline__ pf32x4 mfma16(pu32x4 a, pu32x4 b, pf32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ pf32x16 mfma32(pu32x4 a, pu32x4 b, pf32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+  static constexpr float kShift = 0.f;   // see Fp16
+};
+struct Fp16 {
+  typedef _Float16 elem;
+  typedef pf16x8 x8;
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ float up(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+  static __device__ __forceinline__ pf32x4 mfma16(pu32x4 a, pu32x4 b, pf32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ pf32x16 mfma32(pu32x4 a, pu32x4 b, pf32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+  // Probabilities enter the product with V in 16 bits.  fp16 has few exponents
+  // below 1: a long tail of probabilities under 2^-25 would vanish.  They are
+  // scaled by 2^kShift, sum and output alike, and still fit: a probability is
+  // at most 2^kLazy (below) before scaling.
+  static constexpr float kShift = 6.f;
+};
+
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const pf32x2 f = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, typename T::x2));
+}
+
+// The largest over the four 16-lane rows of a wave, lane by lane.
+__device__ __forceinline__ float rows_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+#endif
+
+}  // namespace gvc

@@ -14,6 +14,7 @@ _LIB_PATH = os.environ.get("GVC_LIBRARY") or os.path.join(os.path.dirname(os.pat
 
 GVC_OK, GVC_EINVAL, GVC_ESTATE, GVC_ENOMEM, GVC_EDEVICE = 0, 1, 2, 3, 4
 REDUCE_MEAN, REDUCE_MIN = 0, 1
+BF16, FP16 = 0, 1
 (STATE_H, STATE_K, STATE_V, STATE_HEAD_LOGITS, STATE_VALID, STATE_ROWS, STATE_MARGINS, STATE_TV, STATE_ENTROPY,
  STATE_LAYER_Q) = range(10)
 
@@ -24,7 +25,8 @@ REDUCE_MEAN, REDUCE_MIN = 0, 1
 EXPORTED = ("gvc_sizes", "gvc_init_cache", "gvc_select_static", "gvc_select_static_noalloc", "gvc_step_prefill",
             "gvc_decode_actions",
             "gvc_margin_gate", "gvc_invalidate", "gvc_read_state", "gvc_state_item_bytes", "gvc_profile_begin",
-            "gvc_profile_end", "gvc_destroy", "gvc_last_error", "gvc_check_rows")
+            "gvc_profile_end", "gvc_destroy", "gvc_last_error", "gvc_check_rows", "gvc_paged_append",
+            "gvc_paged_workspace", "gvc_paged_decode", "gvc_paged_prefill", "gvc_paged_check")
 
 
 class GvcError(RuntimeError):
@@ -66,6 +68,17 @@ class Weights(ctypes.Structure):
                 ("vit", ctypes.POINTER(VitWeights))]
 
 
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_heads", "n_kv_heads", "head_dim", "page_size", "n_pages",
+                                              "n_seqs", "max_pages")]
+
+
+class PagedRope(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int32 * 3), ("theta", ctypes.c_float), ("rms_eps", ctypes.c_float),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("position_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -96,6 +109,13 @@ def lib():
         L.gvc_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
         L.gvc_destroy.argtypes = [vp]
         L.gvc_check_rows.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        pd, f32, i64 = ctypes.POINTER(PagedDesc), ctypes.c_float, ctypes.c_int64
+        L.gvc_paged_append.argtypes = [pd, ctypes.POINTER(PagedRope), vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp,
+                                       vp, i64, vp]
+        L.gvc_paged_workspace.argtypes = [pd, i32, i32, ctypes.POINTER(sz)]
+        L.gvc_paged_decode.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.gvc_paged_prefill.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.gvc_paged_check.argtypes = [pd, vp, vp, vp, vp, i32]
         L.gvc_last_error.restype = ctypes.c_char_p
         for n in EXPORTED:
             if n not in ("gvc_state_item_bytes", "gvc_last_error"):
@@ -194,3 +214,36 @@ def profile_end(ctx: int):
 
 def destroy(ctx: int):
     _check(lib().gvc_destroy(ctx))
+
+
+# ---- the paged cache (gvc_paged_*): device addresses as integers, strides in elements
+def paged_append(desc: PagedDesc, rope: PagedRope, q, q_stride: int, k: int, k_stride: int, v: int, v_stride: int,
+                 row_seq: int, row_slot: int, n_rows: int, k_pages: int, v_pages: int, page_table: int, q_out,
+                 q_out_stride: int, stream: int):
+    _check(lib().gvc_paged_append(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows, k_pages,
+                                  v_pages, page_table, q_out, q_out_stride, stream))
+
+
+def paged_workspace(desc: PagedDesc, prefill: bool, n_rows: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().gvc_paged_workspace(desc, int(prefill), n_rows, ctypes.byref(n)))
+    return n.value
+
+
+def paged_decode(desc: PagedDesc, scale: float, window: int, n_sinks: int, q: int, q_stride: int, lengths: int,
+                 k_pages: int, v_pages: int, page_table: int, out: int, out_stride: int, workspace, workspace_bytes: int,
+                 stream: int):
+    _check(lib().gvc_paged_decode(desc, scale, window, n_sinks, q, q_stride, lengths, k_pages, v_pages, page_table, out,
+                                  out_stride, workspace, workspace_bytes, stream))
+
+
+def paged_prefill(desc: PagedDesc, scale: float, window: int, n_sinks: int, q: int, q_stride: int, row_last: int,
+                  row_begin: int, n_rows: int, k_pages: int, v_pages: int, page_table: int, out: int, out_stride: int,
+                  workspace, workspace_bytes: int, stream: int):
+    _check(lib().gvc_paged_prefill(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages,
+                                   v_pages, page_table, out, out_stride, workspace, workspace_bytes, stream))
+
+
+def paged_check(desc: PagedDesc, page_table: int, lengths, row_seq, row_slot, n_rows: int):
+    """Host-side check (all arguments host addresses, lengths and rows may be None); raises GvcError on a fault."""
+    _check(lib().gvc_paged_check(desc, page_table, lengths, row_seq, row_slot, n_rows))
