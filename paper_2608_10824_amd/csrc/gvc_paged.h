@@ -46,6 +46,15 @@ struct PagedAttnArgs {
   float scale_log2e;      // scores in powers of two
 };
 
+// How a call is cut into units of work, and the workspace of their partial results.
+struct PagedSplit {
+  bool split;       // a row's slots may be split over units (a second launch joins them)
+  int64_t units;    // an upper bound: the grid
+  size_t bytes;
+};
+PagedSplit paged_decode_split(const PagedPool& p, int window, int n_sinks);
+
+hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s);
 hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, hipStream_t s);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, hipStream_t s);
 
@@ -60,6 +69,10 @@ typedef uint32_t pu32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t pu32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t pu16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t pu16x8 __attribute__((ext_vector_type(8)));
+
+// The running maximum may lag behind the true one by 2^kPagedLazy before output
+// and sum are rescaled: a probability is at most 2^kPagedLazy, far from overflow.
+constexpr float kPagedLazy = 8.f;
 
 // The two 16-bit types.  Conversions to 16 bits round to nearest even.
 struct Bf16 {
@@ -89,7 +102,7 @@ struct Fp16 {
   // Probabilities enter the product with V in 16 bits.  fp16 has few exponents
   // below 1: a long tail of probabilities under 2^-25 would vanish.  They are
   // scaled by 2^kShift, sum and output alike, and still fit: a probability is
-  // at most 2^kLazy (below) before scaling.
+  // at most 2^kPagedLazy before scaling.
   static constexpr float kShift = 6.f;
 };
 

@@ -12,9 +12,6 @@
 namespace gvc {
 
 constexpr int kAttnThreads = 256;
-// The running maximum may lag behind the true one by 2^kLazy before output and
-// sum are rescaled: a probability is at most 2^kLazy, far from overflow.
-constexpr float kLazy = 8.f;
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
@@ -97,7 +94,7 @@ __device__ __forceinline__ void visit16(const PagedAttnArgs& a, int seq, int kvh
       x[u] = (seen >> u) & 1 ? s[u >> 2][u & 3] * a.scale_log2e : -INFINITY;
       top = fmaxf(top, x[u]);
     }
-    if (__any(top > st.m + kLazy)) {
+    if (__any(top > st.m + kPagedLazy)) {
       const float mn = fmaxf(st.m, rows_max(top));
       const float nb = mn == -INFINITY ? 0.f : mn;
       const float f = __builtin_amdgcn_exp2f(st.m - nb);
