@@ -383,7 +383,8 @@ typedef struct gvc_paged_desc {
   int32_t page_size;      /* slots of a page: 16, 32, 64 or 128 */
   int32_t n_pages;        /* pages of the pool, >= 1 */
   int32_t n_seqs;         /* rows of the page table, 1 to 4096 */
-  int32_t max_pages;      /* entries of a page-table row; max_pages * page_size <= 2^30 */
+  int32_t max_pages;      /* entries of a page-table row; max_pages * page_size <= 2^30, n_seqs *
+                             max_pages <= 2^27 */
 } gvc_paged_desc;
 
 /* Norm and rotation of gvc_paged_append.  With gains, each head x of q (of k)

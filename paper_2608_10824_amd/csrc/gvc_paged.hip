@@ -33,6 +33,7 @@ const char* bad_desc(const gvc_paged_desc* d) noexcept {
   if (d->n_seqs < 1 || d->n_seqs > kPagedMaxSeqs) return "n_seqs must be in [1, 4096]";
   if (d->max_pages < 1 || (int64_t)d->max_pages * d->page_size > kMaxSlots)
     return "max_pages * page_size must be in [1, 2^30]";
+  if ((int64_t)d->n_seqs * d->max_pages > 1 << 27) return "n_seqs * max_pages must be at most 2^27";
   return nullptr;
 }
 

@@ -22,9 +22,13 @@
 
 namespace gvc {
 
-constexpr int kDecWaves = 8;
-constexpr int kDecMinChunk = 16;   // tiles: shorter sequences are not split
-constexpr int kDecTarget = 1024;   // units that the chunk length aims at, four to a compute unit
+// Waves of a workgroup; three fit a compute unit, and their starts, ends and
+// loads overlap.  (One workgroup of 12 waves instead was slower at every size:
+// 8.6 us against 7.3 for one sequence of 282 slots, 137 against 101 for 131072.)
+constexpr int NW = 4;
+// Units that the chunk length aims at (768 or 2048: 5% slower at one size or
+// another), and the least tiles of a chunk: shorter sequences are not split.
+constexpr int kDecTarget = 1024, kDecMinChunk = 16;
 
 // v, which is the same in every lane, as a scalar: loops and branches on it stay scalar.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -44,66 +48,86 @@ __device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int s) {
   return t;
 }
 
-__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(v, m);
-    if (lane >= m) v += o;
-  }
+// Inclusive sum over the lanes of a wave, on DPP row shifts and broadcasts.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // within rows of 16: 1, 2, 4, 8 lanes down
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // the last lane of rows 0 and 2 to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // the last lane of row 1 to rows 2 and 3
   return v;
-}
-
-// Tiles per chunk: the sum of the tiles over the units aimed at, in whole
-// rounds of the workgroup's waves.  The same in every wave of both launches.
-__device__ __forceinline__ int chunk_tiles(const PagedAttnArgs& a, int heads, int lane) {
-  int total = 0;
-  for (int s = lane; s < a.pool.n_seqs; s += 64) total += min(seq_tiles(a, s).tiles, 1 << 18);
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
-  const long long c = ((long long)total * heads + kDecTarget - 1) / kDecTarget;
-  return uniform(max((int)((c + kDecWaves - 1) / kDecWaves) * kDecWaves, kDecMinChunk));
 }
 
 __device__ __forceinline__ int chunks_of(int tiles, int chunk) { return max((tiles + chunk - 1) / chunk, 1); }
 
+// A unit of a call: chunk `index` of the `count` of sequence seq (-1: past the last one).
+struct Unit {
+  int seq, index, count, chunk;
+  SeqTiles st;
+};
+
+// The chunk length is the sum of all tiles over the units aimed at, in whole
+// rounds of the workgroup's waves (so no sequence has more chunks than that,
+// and one); chunk numbers go through the sequences in
+// order.  Every wave finds this out by itself.
+__device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int heads, int number, int lane) {
+  const int S = a.pool.n_seqs;
+  SeqTiles t = seq_tiles(a, min(lane, S - 1));
+  int total = lane < S ? t.tiles : 0;   // at most 2^29: n_seqs * max_pages <= 2^27
+  for (int s = lane + 64; s < S; s += 64) total += seq_tiles(a, s).tiles;
+  total = __builtin_amdgcn_readlane(wave_scan(total), 63);
+  const long long c = ((long long)total * heads + kDecTarget - 1) / kDecTarget;
+  Unit u{-1, 0, 0, max((int)((c + NW - 1) / NW) * NW, kDecMinChunk), {}};
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    if (s0) t = seq_tiles(a, min(s0 + lane, S - 1));
+    const int n = s0 + lane < S ? chunks_of(t.tiles, u.chunk) : 0;
+    const int sum = wave_scan(n);
+    const uint64_t past = __ballot(sum > number);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      u.seq = s0 + l;
+      u.count = __builtin_amdgcn_readlane(n, l);
+      u.index = number - (__builtin_amdgcn_readlane(sum, l) - u.count);
+      u.st = {__builtin_amdgcn_readlane(t.last, l), __builtin_amdgcn_readlane(t.sink_tiles, l),
+              __builtin_amdgcn_readlane(t.win_tile, l), __builtin_amdgcn_readlane(t.tiles, l)};
+      break;
+    }
+    number -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  u.seq = uniform(u.seq);
+  u.index = uniform(u.index);
+  u.count = uniform(u.count);
+  u.st = {uniform(u.st.last), uniform(u.st.sink_tiles), uniform(u.st.win_tile), uniform(u.st.tiles)};
+  return u;
+}
+
+// A split call's workspace: for each sequence the number of its first chunk
+// and how many it has, then [chunk][key-value head, block of 16 queries][query]
+// [DH + 4] floats: maximum, sum, whether a slot was seen, nothing, output.
+__host__ __device__ __forceinline__ int64_t plan_bytes(int n_seqs) { return ((int64_t)n_seqs * 8 + 15) / 16 * 16; }
+
 template <class T, int DH>
-__global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedAttnArgs a, float* part) {
+__global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs a, char* work) {
   constexpr int NK = DH / 32, NO = DH / 16;
   extern __shared__ float lds[];   // [waves / 2][queries][DH + 4], then [waves][16][4]
   const PagedPool& p = a.pool;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int G = p.H / p.Hk, blocks = (G + 15) >> 4, heads = p.Hk * blocks;
-  const int chunk = chunk_tiles(a, heads, lane);
-  // the sequence of this workgroup's chunk
-  const int head = blockIdx.x % heads;
-  int want = blockIdx.x / heads, seq = -1, c_idx = 0, n_chunks = 0;
-  for (int s0 = 0; s0 < p.n_seqs && seq < 0; s0 += 64) {
-    const int s = s0 + lane;
-    const int n = s < p.n_seqs ? chunks_of(seq_tiles(a, s).tiles, chunk) : 0;
-    const int sum = wave_scan(n, lane);
-    const uint64_t past = __ballot(sum > want);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      seq = s0 + l;
-      n_chunks = __builtin_amdgcn_readlane(n, l);
-      c_idx = want - (__builtin_amdgcn_readlane(sum, l) - n_chunks);
-    } else {
-      want -= __builtin_amdgcn_readlane(sum, 63);
-    }
-  }
-  seq = uniform(seq);
-  if (seq < 0) return;   // the grid is an upper bound; uniform over the workgroup
-  c_idx = uniform(c_idx);
-  n_chunks = uniform(n_chunks);
-  SeqTiles st = seq_tiles(a, seq);
-  st = {uniform(st.last), uniform(st.sink_tiles), uniform(st.win_tile), uniform(st.tiles)};
-  const int t_end = min((c_idx + 1) * chunk, st.tiles);
+  const int head = blockIdx.x % heads, number = blockIdx.x / heads;
+  const Unit unit = find_unit(a, heads, number, lane);
+  if (unit.seq < 0) return;   // the grid is an upper bound; uniform over the workgroup
+  const SeqTiles& st = unit.st;
+  const int seq = unit.seq, t_end = min((unit.index + 1) * unit.chunk, st.tiles);
+  if (work && head == 0 && unit.index == 0 && threadIdx.x == 0) ((int2*)work)[seq] = int2{number, unit.count};
   const int kvh = head / blocks, hb = head % blocks;
   const int qs = min(G - hb * 16, 16), h0 = kvh * G + hb * 16;
   const int* table = p.table + (int64_t)seq * p.max_pages;
   const int in_page = (1 << p.page_shift) - 1;
   auto tile_slot = [&](int t) { return 32 * (t < st.sink_tiles ? t : t - st.sink_tiles + st.win_tile); };
+
+  const int lo = a.window ? st.last - a.window : -1;   // slots past lo are in the window
 
   pu32x4 qf[NK];
 #pragma unroll
@@ -117,18 +141,20 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
   float m = -INFINITY, mb = T::kShift, l = 0.f;   // maximum, what a score is shifted by, this lane's share of the sum
   unsigned any = 0;
 
-  // The wave's tiles t0, t0 + waves, ...: page ids of 32 of them at a time, one
+  // The wave's tiles go round the waves.  Page ids of 32 of them at a time, one
   // half tile (16 slots, always one page) to a lane.
+  const int t0 = unit.index * unit.chunk + wv;
   int ids = -1, ids_base = 0;
-  const int t0 = c_idx * chunk + wv;
   auto load_ids = [&](int n) {   // of the wave's tiles n .. n + 31
-    const int t = t0 + (n + (lane >> 1)) * kDecWaves;
+    const int t = t0 + (n + (lane >> 1)) * NW;
     const int j = tile_slot(min(t, max(t_end - 1, 0))) + 16 * (lane & 1);
     const int id = table[min(j >> p.page_shift, p.max_pages - 1)];
     ids = (unsigned)id < (unsigned)p.n_pages ? id : -1;
     ids_base = n;
   };
-  // operands of tile t, the wave's n-th: keys in rows 4 g' + i of operand e are slots 8 g' + 4 e + i
+  // Operands of tile t, if there is one more; else the start of the pool, once
+  // for all lanes: a branch around the loads would cost the waits for them
+  // their order.  Keys in rows 4 g' + i of operand e are slots 8 g' + 4 e + i
   pu32x4 kf[2][NK], vf[NO];
   int id0, id1;
   auto page_ids = [&](int n) {
@@ -136,45 +162,45 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
     id0 = __builtin_amdgcn_readlane(ids, 2 * (n - ids_base));
     id1 = __builtin_amdgcn_readlane(ids, 2 * (n - ids_base) + 1);
   };
-  auto load_k = [&](int t) {
+  auto load_k = [&](int t, bool more) {
     const int j = (tile_slot(t) & in_page) + 8 * (col >> 2) + (col & 3);   // slot of the lane's row in the pages of the tile
     const int64_t b0 = ((int64_t)max(id0, 0) * p.Hk + kvh) << p.page_shift, b1 = ((int64_t)max(id1, 0) * p.Hk + kvh) << p.page_shift;
-    const uint16_t* kp = p.k + ((col < 8 ? b0 : b1) + (j & in_page)) * DH + g * 8;
+    const int64_t at = ((col < 8 ? b0 : b1) + (j & in_page)) * DH + g * 8;
+    const uint16_t* kp = p.k + (more ? at : 0);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) kf[e][kk] = *(const pu32x4*)(kp + e * 4 * DH + kk * 32);
   };
-  auto load_v = [&](int t) {
+  auto load_v = [&](int t, bool more) {
     const int j = (tile_slot(t) & in_page) + 8 * g;
     const int64_t b0 = ((int64_t)max(id0, 0) * p.Hk + kvh) * DH, b1 = ((int64_t)max(id1, 0) * p.Hk + kvh) * DH;
-    const uint16_t* vp = p.v + (((g < 2 ? b0 : b1) + col) << p.page_shift) + (j & in_page);
+    const int64_t at = (((g < 2 ? b0 : b1) + col) << p.page_shift) + (j & in_page);
+    const uint16_t* vp = p.v + (more ? at : 0);
 #pragma unroll
     for (int c = 0; c < NO; ++c) vf[c] = *(const pu32x4*)(vp + ((16 * c) << p.page_shift));
   };
   if (t0 < t_end) {
     load_ids(0);
     page_ids(0);
-    load_k(t0);
-    // K before V here as in the loop, or every wait for K would wait for V as well
+    load_k(t0, true);
+    // K before V here as in the loop, or every wait for K there would wait for V as well
     __builtin_amdgcn_sched_barrier(0);
-    load_v(t0);
+    load_v(t0, true);
   }
-  int n = 0;
-  for (int t = t0; t < t_end; t += kDecWaves, ++n) {
-    const int j0 = tile_slot(t);
+  // The next tile's K are loaded as soon as the scores are done, its V after the second product.
+  for (int t = t0, n = 0; t < t_end; ++n) {
+    const int j0 = tile_slot(t), next = t + NW;
+    const bool more = next < t_end;
     const bool okv = (g < 2 ? id0 : id1) >= 0;
-    const bool full = id0 >= 0 && id1 >= 0 && j0 + 31 <= st.last && (a.window == 0 || j0 > st.last - a.window);
-    const bool more = t + kDecWaves < t_end;
+    const bool full = id0 >= 0 && id1 >= 0 && j0 + 31 <= st.last && j0 > lo;
     pf32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
       for (int e = 0; e < 2; ++e) s[e] = T::mfma16(kf[e][kk], qf[kk], s[e]);
-    if (more) {
-      page_ids(n + 1);
-      load_k(t + kDecWaves);   // in flight over the softmax and the second product
-    }
+    if (more) page_ids(n + 1);
+    load_k(next, more);
     float x[8], top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 8; ++u) x[u] = s[u >> 2][u & 3];
@@ -185,7 +211,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int j = j0 + 8 * g + u;
-        const bool in = okv && j <= st.last && (a.window == 0 || j > st.last - a.window || j < a.n_sinks);
+        const bool in = okv & (j <= st.last) & ((j > lo) | (j < a.n_sinks));
         x[u] = in ? x[u] : -INFINITY;
         seen |= (unsigned)in << u;
       }
@@ -217,13 +243,14 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
     const pu32x4 pf = {pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])};
 #pragma unroll
     for (int c = 0; c < NO; ++c) acc[c] = T::mfma16(vf[c], pf, acc[c]);
-    if (more) load_v(t + kDecWaves);
+    t = next;
+    load_v(t, more);
   }
 
   // Join the waves: every wave scales its output to the common maximum; the
   // second half of them adds theirs to the first half's through LDS, then all
   // threads add up what is left.
-  constexpr int kHalf = kDecWaves / 2;
+  constexpr int kHalf = NW / 2;
   const int row = DH + 4;   // floats between queries: four apart in banks
   float* ml = lds + kHalf * qs * row;
   l = rows_sum(l);
@@ -232,7 +259,7 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
   __syncthreads();
   float mm = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kDecWaves; ++w) mm = fmaxf(mm, ml[(w * 16 + col) * 4]);
+  for (int w = 0; w < NW; ++w) mm = fmaxf(mm, ml[(w * 16 + col) * 4]);
   const float mine = __builtin_amdgcn_exp2f(m - (mm == -INFINITY ? 0.f : mm));
 #pragma unroll
   for (int c = 0; c < NO; ++c) acc[c] *= mine;
@@ -245,14 +272,14 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
 #pragma unroll
     for (int c = 0; c < NO; ++c) *(pf32x4*)(o_row + 16 * c) = acc[c] + *(const pf32x4*)(o_row + 16 * c);
   __syncthreads();
-  for (int i = threadIdx.x; i < qs * (DH / 4); i += kDecWaves * 64) {
+  for (int i = threadIdx.x; i < qs * (DH / 4); i += NW * 64) {
     const int q = i / (DH / 4), d = i % (DH / 4) * 4;
     float top = -INFINITY, ll = 0.f, saw = 0.f;
 #pragma unroll
-    for (int w = 0; w < kDecWaves; ++w) top = fmaxf(top, ml[(w * 16 + q) * 4]);
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ml[(w * 16 + q) * 4]);
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int w = 0; w < kDecWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const pf32x4 x = *(const pf32x4*)(ml + (w * 16 + q) * 4);
       ll += x[1] * __builtin_amdgcn_exp2f(x[0] - ref);
       saw += x[2];
@@ -260,93 +287,110 @@ __global__ __launch_bounds__(kDecWaves * 64, 2) void k_paged_decode(const PagedA
     pf32x4 o = {0, 0, 0, 0};
 #pragma unroll
     for (int w = 0; w < kHalf; ++w) o += *(const pf32x4*)(lds + (w * qs + q) * row + d);
-    if (n_chunks == 1) {
+    if (unit.count == 1) {
       const float inv = 1.f / ll;
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
       *(pu32x2*)(a.out + seq * a.out_stride + (h0 + q) * DH + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
     } else {
-      float* to = part + ((int64_t)blockIdx.x * min(G, 16) + q) * row;
+      float* to = (float*)(work + plan_bytes(p.n_seqs)) + ((int64_t)blockIdx.x * min(G, 16) + q) * row;
       *(pf32x4*)(to + 4 + d) = o;
       if (d == 0) *(pf32x4*)to = pf32x4{top, ll, saw, 0.f};
     }
   }
 }
 
-// Joins the chunks of a sequence: a wave per query head, a workgroup's waves
-// taking chunks round robin.
-constexpr int kJoinWaves = 4;
-template <class T, int DH>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_paged_join(const PagedAttnArgs a, const float* part) {
-  __shared__ float o_w[kJoinWaves][DH], ml_w[kJoinWaves][3];
+// Joins the chunks of a sequence: a workgroup for each query head.  Weights of
+// the chunks from their maxima, then groups of DH / 4 threads add up the
+// weighted outputs of every n-th chunk, and the groups' sums are added in LDS.
+template <class T, int DH, int NT>
+__global__ __launch_bounds__(NT) void k_paged_join(const PagedAttnArgs a, const char* work) {
+  constexpr int GT = DH / 4, NG = NT / GT;
+  __shared__ float weight[kDecTarget + 1], sums[3][NT / 64];
+  __shared__ pf32x4 part_o[NG][GT];
   const PagedPool& p = a.pool;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int G = p.H / p.Hk, blocks = (G + 15) >> 4, heads = p.Hk * blocks;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int seq = blockIdx.x / p.H, h = blockIdx.x % p.H;
-  const int chunk = chunk_tiles(a, heads, lane);
-  const int n = chunks_of(seq_tiles(a, seq).tiles, chunk);
-  if (n == 1) return;   // the unit has written the output
-  int before = 0;       // chunks of earlier sequences
-  for (int s = lane; s < seq; s += 64) before += chunks_of(seq_tiles(a, s).tiles, chunk);
+  const int2 plan = ((const int2*)work)[seq];
+  const int n = plan.y;
+  if (n == 1) return;   // the unit has written the output; uniform
+  const int G = p.H / p.Hk, blocks = (G + 15) >> 4, heads = p.Hk * blocks;
+  const int head = h / G * blocks + h % G / 16, q = h % G % 16, wide = min(G, 16);
+  const float* from = (const float*)(work + plan_bytes(p.n_seqs)) + (((int64_t)plan.x * heads + head) * wide + q) * (DH + 4);
+  const int64_t step = (int64_t)heads * wide * (DH + 4);   // floats between chunks
+  float m = -INFINITY;
+  for (int c = tid; c < n; c += NT) {
+    weight[c] = from[c * step];
+    m = fmaxf(m, weight[c]);
+  }
+  m = fmaxf(m, __shfl_xor(m, 1));
+  m = fmaxf(m, __shfl_xor(m, 2));
+  m = fmaxf(m, __shfl_xor(m, 4));
+  m = fmaxf(m, __shfl_xor(m, 8));
+  m = rows_max(m);
+  if (lane == 0) sums[0][wv] = m;
+  __syncthreads();
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) before += __shfl_xor(before, k);
-  const int head = h / G * blocks + h % G / 16, q = h % G % 16, row = DH + 4, wide = min(G, 16);
-  constexpr int D = DH / 64;   // dimensions of a lane
-  float m = -INFINITY, l = 0.f, saw = 0.f, o[D] = {};
-  for (int c = wv; c < n; c += kJoinWaves) {
-    const float* from = part + (((int64_t)(before + c) * heads + head) * wide + q) * row;
-    const pf32x4 x = *(const pf32x4*)from;
-    const float mn = fmaxf(m, x[0]), ref = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f(m - ref), e = __builtin_amdgcn_exp2f(x[0] - ref);
-    m = mn;
-    l = l * f + x[1] * e;
-    saw += x[2];
-#pragma unroll
-    for (int d = 0; d < D; ++d) o[d] = o[d] * f + from[4 + lane * D + d] * e;
+  for (int w = 0; w < NT / 64; ++w) m = fmaxf(m, sums[0][w]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, saw = 0.f;
+  for (int c = tid; c < n; c += NT) {
+    const float f = __builtin_amdgcn_exp2f(weight[c] - ref);
+    weight[c] = f;
+    l += from[c * step + 1] * f;
+    saw += from[c * step + 2];
   }
 #pragma unroll
-  for (int d = 0; d < D; ++d) o_w[wv][lane * D + d] = o[d];
-  if (lane == 0) ml_w[wv][0] = m, ml_w[wv][1] = l, ml_w[wv][2] = saw;
+  for (int k = 1; k < 16; k <<= 1) {
+    l += __shfl_xor(l, k);
+    saw += __shfl_xor(saw, k);
+  }
+  l = rows_sum(l);
+  saw = rows_sum(saw);
+  if (lane == 0) sums[1][wv] = l, sums[2][wv] = saw;
   __syncthreads();
-  if (threadIdx.x >= DH / 2) return;
-  m = -INFINITY;
+  const int gr = tid / GT, d = tid % GT;
+  pf32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int c = gr; c < n; c += NG) o += *(const pf32x4*)(from + c * step + 4 + 4 * d) * weight[c];
+  part_o[gr][d] = o;
+  __syncthreads();
+  if (tid >= GT) return;
+  o = part_o[0][d];
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) m = fmaxf(m, ml_w[w][0]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float x = 0.f, y = 0.f;
+  for (int k = 1; k < NG; ++k) o += part_o[k][d];
   l = saw = 0.f;
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) {
-    const float f = __builtin_amdgcn_exp2f(ml_w[w][0] - ref);
-    l += ml_w[w][1] * f;
-    saw += ml_w[w][2];
-    x += o_w[w][2 * threadIdx.x] * f;
-    y += o_w[w][2 * threadIdx.x + 1] * f;
-  }
+  for (int w = 0; w < NT / 64; ++w) l += sums[1][w], saw += sums[2][w];
   const float inv = 1.f / l;
-  x = saw > 0.f ? x * inv : 0.f;
-  y = saw > 0.f ? y * inv : 0.f;
-  *(uint32_t*)(a.out + seq * a.out_stride + h * DH + 2 * threadIdx.x) = pack2<T>(x, y);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
+  *(pu32x2*)(a.out + seq * a.out_stride + h * DH + 4 * d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
 }
 
 PagedSplit paged_decode_split(const PagedPool& p, int window, int n_sinks) {
   const int G = p.H / p.Hk, heads = p.Hk * ((G + 15) / 16);
-  PagedSplit s{};
   // the most tiles that a token can see
   const int64_t slots = (int64_t)p.max_pages << p.page_shift, all = (slots + 31) / 32;
   const int64_t seen = window ? ((int64_t)window + 31) / 32 + 1 + ((int64_t)n_sinks + 31) / 32 : all;
+  PagedSplit s{};
   s.split = (seen < all ? seen : all) > kDecMinChunk;
   s.units = (int64_t)p.n_seqs * heads + (s.split ? kDecTarget : 0);
-  s.bytes = s.split ? (size_t)s.units * (G < 16 ? G : 16) * (p.dh + 4) * sizeof(float) : 0;
+  s.bytes = s.split ? (size_t)(plan_bytes(p.n_seqs) + s.units * (G < 16 ? G : 16) * (p.dh + 4) * (int64_t)sizeof(float)) : 0;
   return s;
 }
 
 template <class T, int DH>
 static hipError_t decode(const PagedAttnArgs& a, const PagedSplit& sp, void* workspace, hipStream_t s) {
   const int G = a.pool.H / a.pool.Hk, wide = G < 16 ? G : 16;
-  const size_t lds = (size_t)kDecWaves * (wide * (DH + 4) / 2 + 16 * 4) * sizeof(float);
-  k_paged_decode<T, DH><<<(unsigned)sp.units, kDecWaves * 64, lds, s>>>(a, (float*)workspace);
-  if (sp.split) k_paged_join<T, DH><<<a.pool.n_seqs * a.pool.H, kJoinWaves * 64, 0, s>>>(a, (const float*)workspace);
+  const size_t lds = (size_t)NW * (wide * (DH + 4) / 2 + 16 * 4) * sizeof(float);
+  char* work = sp.split ? (char*)workspace : nullptr;
+  k_paged_decode<T, DH><<<(unsigned)sp.units, NW * 64, lds, s>>>(a, work);
+  if (sp.split) {
+    const unsigned rows = a.pool.n_seqs * a.pool.H;
+    if (rows <= 256) k_paged_join<T, DH, 1024><<<rows, 1024, 0, s>>>(a, work);   // many chunks each
+    else k_paged_join<T, DH, 256><<<rows, 256, 0, s>>>(a, work);
+  }
   return hipGetLastError();
 }
 

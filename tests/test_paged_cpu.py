@@ -100,6 +100,15 @@ def test_bad_lists_refused():
     _refused(_prefill, _desc(), n=1 << 27)
 
 
+def test_largest_tables():
+    """2^30 slots in a row of the table and 2^27 entries in all are the most."""
+    from paper_2608_10824_amd import gvc
+    assert gvc.paged_workspace(_desc(n_seqs=4096, max_pages=1 << 15), False, 4096) > 0
+    assert gvc.paged_workspace(_desc(n_seqs=1, max_pages=1 << 26), False, 1) > 0
+    _refused(gvc.paged_workspace, _desc(n_seqs=4096, max_pages=(1 << 15) + 1), False, 4096)
+    _refused(gvc.paged_workspace, _desc(n_seqs=1, max_pages=(1 << 26) + 1), False, 1)
+
+
 def test_norm_gains_and_positions_refused():
     r = _rope()
     r.q_norm = P + 2
