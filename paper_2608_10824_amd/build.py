@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgvc.so")
 SOURCES = ["k_tile.hip", "k_gemm.hip", "k_select.hip", "k_misc.hip", "k_attn.hip", "k_decode.hip",
-           "k_paged_append.hip", "k_paged_attn.hip", "k_paged_decode.hip", "gvc_paged.hip", "gvc_api.hip"]
+           "k_paged_append.hip", "k_paged_decode.hip", "k_paged_prefill.hip", "gvc_paged.hip", "gvc_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -4,6 +4,7 @@
 #include "gvc.h"
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace gvc {
 
@@ -50,13 +51,16 @@ struct PagedAttnArgs {
 struct PagedSplit {
   bool split;       // a row's slots may be split over units (a second launch joins them)
   int64_t units;    // an upper bound: the grid
+  int64_t tiles;    // prefill: row tiles, at most, and the parts that each one's slots are cut into
+  int parts;
   size_t bytes;
 };
 PagedSplit paged_decode_split(const PagedPool& p, int window, int n_sinks);
+PagedSplit paged_prefill_split(const PagedPool& p, int n_rows);
 
 hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s);
+hipError_t launch_paged_prefill(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s);
 hipError_t launch_paged_append(const PagedAppendArgs& a, int dtype, hipStream_t s);
-hipError_t launch_paged_attn(const PagedAttnArgs& a, int dtype, hipStream_t s);
 
 #ifdef __HIPCC__
 // ------------------------------------------------------------------ device

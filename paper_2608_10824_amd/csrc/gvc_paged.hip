@@ -88,11 +88,12 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.window = window >= slots ? 0 : window;   // a window over every slot hides none
   a.n_sinks = (int)std::min<int64_t>(n_sinks, slots);
   a.scale_log2e = scale * 1.44269504088896340736f;
-  if (row_begin) return device(launch_paged_attn(a, d.dtype, static_cast<hipStream_t>(stream)));
-  const PagedSplit sp = paged_decode_split(a.pool, a.window, a.n_sinks);
+  const PagedSplit sp = row_begin ? paged_prefill_split(a.pool, n_rows) : paged_decode_split(a.pool, a.window, a.n_sinks);
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))
     return set_error(GVC_ENOMEM, "the workspace is too small (or not 16-byte aligned)");
-  return device(launch_paged_decode(a, sp, d.dtype, workspace, static_cast<hipStream_t>(stream)));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return device(row_begin ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
+                          : launch_paged_decode(a, sp, d.dtype, workspace, s));
 }
 
 }  // namespace
@@ -159,7 +160,8 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
 int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, size_t* bytes) {
   if (const char* w = bad_desc(desc)) return fail(w);
   if (!bytes || n_rows < 0) return fail("null bytes or negative n_rows");
-  *bytes = prefill ? 0 : paged_decode_split(pool_of(*desc, nullptr, nullptr, nullptr), 0, 0).bytes;
+  const PagedPool p = pool_of(*desc, nullptr, nullptr, nullptr);
+  *bytes = prefill ? paged_prefill_split(p, n_rows).bytes : paged_decode_split(p, 0, 0).bytes;
   return GVC_OK;
 }
 

@@ -1,0 +1,405 @@
+// Attention of lists of rows over the paged cache.
+//
+// The query heads that share a key-value head count as rows: virtual row v of
+// a sequence is row v / G, head v % G of the group.  A workgroup takes 128 of
+// them, 32 to a wave, and goes through the slots that some of them see in
+// tiles of 64, which are copied once for its waves straight into LDS, one tile
+// ahead.  Long lists are bound by the matrix cores and the softmax between the
+// two products.  S^T = K Q^T and O^T += V^T P^T run on 32x32x16 MFMA: a lane's
+// scores are of one query, and the keys of a tile are taken in an order in
+// which they are also the lane's operand of the second product, so
+// probabilities stay in registers and a row's maximum and sum need one
+// exchange between two lanes.
+//
+// Tiles of late rows see the most slots and start first.  Neighbouring
+// workgroups take different key-value heads, so an XCD's L2 holds the keys and
+// values of few heads.  Few rows over many slots are split over the slots as
+// well; a second launch joins the parts.
+#include "gvc_paged.h"
+#include "gvc_sync.h"
+
+#define GPA(p) ((const void __attribute__((address_space(1)))*)(p))
+#define LPA(p) ((void __attribute__((address_space(3)))*)(p))
+
+namespace gvc {
+
+constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves, kPreKeys = 64;
+constexpr int kPreUnits = 512;   // calls with fewer units split the slots, into about twice as many
+constexpr int kPreMinTiles = 4;  // tiles of a part, at least
+
+__device__ __forceinline__ int uniform32(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The tile of virtual rows that a workgroup takes.
+struct RowTile {
+  int seq, first, begin, rows;   // sequence (-1: none), the tile's first virtual row, the sequence's first row, its virtual rows
+};
+
+__device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int s, int& begin) {
+  begin = min(max(a.row_begin[s], 0), a.n_rows);
+  return max(min(a.row_begin[s + 1], a.n_rows) - begin, 0);
+}
+
+__device__ __forceinline__ int scan64(int v, int lane) {   // inclusive
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(v, m);
+    if (lane >= m) v += o;
+  }
+  return v;
+}
+
+// Tile `number` of the call, counted from the last sequence's last rows.
+__device__ __forceinline__ RowTile find_tile(const PagedAttnArgs& a, int G, int number, int lane) {
+  RowTile t{-1, 0, 0, 0};
+  for (int s1 = a.pool.n_seqs; s1 > 0; s1 -= 64) {
+    const int s = s1 - 1 - lane;
+    int begin = 0;
+    const int rows = s >= 0 ? rows_of(a, s, begin) * G : 0;
+    const int n = (rows + kPreRows - 1) / kPreRows;
+    const int sum = scan64(n, lane);
+    const uint64_t past = __ballot(sum > number);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      t.seq = s1 - 1 - l;
+      t.begin = __builtin_amdgcn_readlane(begin, l);
+      t.rows = __builtin_amdgcn_readlane(rows, l);
+      t.first = (__builtin_amdgcn_readlane(sum, l) - 1 - number) * kPreRows;
+      break;
+    }
+    number -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return {uniform32(t.seq), uniform32(t.first), uniform32(t.begin), uniform32(t.rows)};
+}
+
+template <class T, int DH>
+__global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const PagedAttnArgs a, float* work, int parts) {
+  constexpr int NK = DH / 16, ND = DH / 32;
+  constexpr int CR = DH / 8;               // 16-byte chunks of a key's row
+  constexpr int RI = 64 / CR;              // keys of one copy (1 KiB)
+  constexpr int KI = 16 / RI;              // copies of K to a wave (16 keys of the tile), and of V (DH / 4 dimensions)
+  constexpr int kTile = kPreKeys * DH * 2; // bytes of K, and of V
+  __shared__ __attribute__((aligned(16))) char lds[2][2][kTile];
+  const PagedPool& p = a.pool;
+  const int lane = threadIdx.x & 63, wv = uniform32(threadIdx.x >> 6);
+  const int r32 = lane & 31, half = lane >> 5;
+  const int G = p.H / p.Hk, kvh = blockIdx.x % p.Hk, part = blockIdx.x / p.Hk % parts;
+  const RowTile rt = find_tile(a, G, blockIdx.x / p.Hk / parts, lane);
+  if (rt.seq < 0) return;   // the grid is an upper bound; uniform over the workgroup
+  const int v = rt.first + wv * 32 + r32;
+  const bool live = v < rt.rows;
+  const int row = rt.begin + min(v, rt.rows - 1) / G, h = kvh * G + min(v, rt.rows - 1) % G;
+  const int slots = p.max_pages << p.page_shift;
+  const int last = live ? min(max(a.row_last[row], -1), slots - 1) : -1;
+  // What the wave's rows see: slots in (lo_some, hi_some] (or below the sinks)
+  // some row, in (lo_all, hi_all] every row; dead rows do not count.
+  int hi_some = last, lo_some = last < 0 ? slots : last, hi_all = live ? last : slots;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    hi_some = max(hi_some, __shfl_xor(hi_some, m));
+    lo_some = min(lo_some, __shfl_xor(lo_some, m));
+    hi_all = min(hi_all, __shfl_xor(hi_all, m));
+  }
+  int* shared_rows = (int*)lds;
+  if (lane == 0) {
+    shared_rows[wv] = hi_some;
+    shared_rows[kPreWaves + wv] = lo_some;
+  }
+  __syncthreads();
+  int hi = shared_rows[0], lo = shared_rows[kPreWaves];
+#pragma unroll
+  for (int w = 1; w < kPreWaves; ++w) {
+    hi = max(hi, shared_rows[w]);
+    lo = min(lo, shared_rows[kPreWaves + w]);
+  }
+  __syncthreads();
+  hi = uniform32(hi);
+  lo = uniform32(lo);
+  const int lo_all = uniform32(a.window ? hi_some - a.window : -1);
+  hi_some = uniform32(hi_some);
+  hi_all = uniform32(hi_all);
+  lo_some = uniform32(a.window ? lo_some - a.window : -1);
+  const int lo_row = a.window ? last - a.window : -1;
+  // the workgroup's tiles: the sinks', then the window's; and this part of them
+  const int end = (hi >> 6) + 1, win_lo = a.window ? max(lo - a.window + 1, 0) >> 6 : 0;
+  const int sink_tiles = a.window ? min((a.n_sinks + 63) >> 6, min(win_lo, end)) : 0;
+  const int win_tile = max(win_lo, sink_tiles);
+  const int tiles = hi < 0 ? 0 : sink_tiles + end - win_tile;
+  const int part_tiles = max((tiles + parts - 1) / parts, kPreMinTiles);
+  const int n_parts = parts == 1 ? 1 : max((tiles + part_tiles - 1) / part_tiles, 1);
+  if (part >= n_parts) return;
+  const int t_begin = parts == 1 ? 0 : part * part_tiles, t_end = parts == 1 ? tiles : min(tiles, t_begin + part_tiles);
+
+  const int* table = p.table + (int64_t)rt.seq * p.max_pages;
+  const int in_page = (1 << p.page_shift) - 1;
+  auto tile_slot = [&](int t) { return 64 * (t < sink_tiles ? t : t - sink_tiles + win_tile); };
+  pu32x4 qf[NK];
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) qf[kk] = *(const pu32x4*)(a.q + row * a.q_stride + h * DH + kk * 16 + half * 8);
+
+  // Copies.  K: LDS row n of a tile holds slot slot_of(n), the order of the
+  // operand's rows; chunk c of it is at c ^ n (mod CR).  V: dimension d's eight
+  // chunks of eight slots, chunk c at c ^ d (mod 8).  So lanes that read an operand
+  // from neighbouring rows hit different banks.
+  auto slot_of = [](int n) { return (n & ~12) | ((n & 4) << 1) | ((n & 8) >> 1); };
+  const int v_chunk = (lane & 7) ^ (lane >> 3);   // of this lane in every copy of V
+  int k_off[KI];   // elements from the page's row of the wave's first slot
+#pragma unroll
+  for (int i = 0; i < KI; ++i) {
+    const int n = i * RI + lane / CR;   // of 16
+    k_off[i] = slot_of(n) * DH + ((lane & (CR - 1)) ^ (n & (CR - 1))) * 8;
+  }
+  auto load_ids = [&](int t) {   // the page of chunk v_chunk of tile t
+    const int j = tile_slot(min(t, t_end - 1)) + 8 * v_chunk;
+    return table[min(j >> p.page_shift, p.max_pages - 1)];
+  };
+  auto copy = [&](int t, int id) {
+    char* to = lds[t & 1][0];
+    const int j0 = tile_slot(t);
+    const int kid = __builtin_amdgcn_readlane(id, 2 * wv);   // lanes 0 to 7 hold chunks 0 to 7
+    const int64_t kb = ((((int64_t)((unsigned)kid < (unsigned)p.n_pages ? kid : 0) * p.Hk + kvh) << p.page_shift) +
+                        ((j0 + 16 * wv) & in_page)) * DH;
+#pragma unroll
+    for (int i = 0; i < KI; ++i)
+      __builtin_amdgcn_global_load_lds(GPA(p.k + kb + k_off[i]), LPA(to + (wv * KI + i) * 1024), 16, 0, 0);
+    const int64_t vb = (((int64_t)((unsigned)id < (unsigned)p.n_pages ? id : 0) * p.Hk + kvh) * DH) << p.page_shift;
+    const uint16_t* vp = p.v + vb + ((wv * KI * 8 + (lane >> 3)) << p.page_shift) + ((j0 + 8 * v_chunk) & in_page);
+#pragma unroll
+    for (int i = 0; i < KI; ++i)
+      __builtin_amdgcn_global_load_lds(GPA(vp + ((8 * i) << p.page_shift)), LPA(to + kTile + (wv * KI + i) * 1024), 16, 0, 0);
+  };
+  // where this lane's operands start
+  int k_at[NK], v_at[4];
+#pragma unroll
+  for (int kk = 0; kk < NK; ++kk) k_at[kk] = r32 * (CR * 16) + (((2 * kk + half) ^ (r32 & (CR - 1))) << 4);
+#pragma unroll
+  for (int m = 0; m < 4; ++m) v_at[m] = kTile + r32 * 128 + (((2 * m + half) ^ (r32 & 7)) << 4);
+
+  pf32x16 acc[ND];
+  float m_run, l_run;   // maximum (powers of two), this lane's share of the sum
+  bool any;
+  // CAREFUL: values in slots that only some rows of the wave see are added slot
+  // by slot, so that NaN and infinities there stay with the rows that see them.
+  auto pass = [&](auto careful) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    m_run = -INFINITY;
+    l_run = 0.f;
+    any = false;
+    float shift = T::kShift;   // a score's exponent is score * scale + shift
+    if (t_begin >= t_end) return;
+    int id = load_ids(t_begin), next_id = load_ids(t_begin + 1);
+    copy(t_begin, id);
+    uint64_t ok = __ballot((unsigned)id < (unsigned)p.n_pages);
+    for (int t = t_begin; t < t_end; ++t) {
+      wait_vmcnt<0>();   // this wave's copies of tile t
+      lds_barrier();     // everyone's, and everyone is done with tile t - 1
+      uint64_t next_ok = 0;
+      if (t + 1 < t_end) {
+        copy(t + 1, next_id);
+        next_ok = __ballot((unsigned)next_id < (unsigned)p.n_pages);
+        next_id = load_ids(t + 2);
+      }
+      const int j0 = tile_slot(t);
+      const unsigned pages = (unsigned)ok & 0xff;   // of the tile's chunks
+      ok = next_ok;
+      if (j0 > hi_some || (j0 + 63 <= lo_some && j0 >= a.n_sinks)) continue;   // nothing for this wave
+      const bool full = pages == 0xff && j0 + 63 <= hi_all && j0 > lo_all;
+      const char* st = lds[t & 1][0];
+      pf32x16 s[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[e][i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+          s[e] = T::mfma32(*(const pu32x4*)(st + k_at[kk] + e * 32 * CR * 16), qf[kk], s[e]);
+      }
+      uint32_t seen = ~0u, some = ~0u;   // element 16 e + i is slot j0 + 32 e + 16 (i / 8) + 8 half + i % 8
+      if (!full) {
+        seen = some = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int c = 2 * (i >> 3) + half, j = j0 + 8 * c + (i & 7);
+          const bool on = (pages >> c) & 1;
+          const bool in = on & (j <= last) & ((j > lo_row) | (j < a.n_sinks));
+          const bool by = on & (j <= hi_some) & ((j > lo_some) | (j < a.n_sinks));
+          s[i >> 4][i & 15] = in ? s[i >> 4][i & 15] : -INFINITY;
+          seen |= (uint32_t)in << i;
+          some |= (uint32_t)by << i;
+        }
+      }
+      any |= seen != 0;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+      top *= a.scale_log2e;   // positive
+      if (__any(top > m_run + kPagedLazy)) {
+        const float mn = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32))), nb = mn == -INFINITY ? 0.f : mn;
+        const float f = __builtin_amdgcn_exp2f(m_run - nb);
+        m_run = mn;
+        shift = T::kShift - nb;
+        l_run *= f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] *= f;
+      }
+      float x[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, shift));
+        l_run += x[i];
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float* y = x + 8 * m;
+        const pu32x4 pf = {pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
+        pu32x4 vf[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[d] = *(const pu32x4*)(st + v_at[m] + d * 32 * 128);
+        if (!full) {   // values that no row of the wave sees become zeros (0 x NaN is NaN)
+          const uint32_t b = some >> (8 * m);
+          pu32x4 keep;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            keep[w] = ((b >> (2 * w)) & 1 ? 0xffffu : 0u) | ((b >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) vf[d] &= keep;
+        }
+        if (!decltype(careful)::value || full) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc[d] = T::mfma32(vf[d], pf, acc[d]);
+        } else {
+          for (int u = 0; u < 16; ++u) {   // slot 16 m + u of the tile: element u % 8 of the lanes with half == u / 8
+            const unsigned bits = (unsigned)__shfl((int)(seen >> (8 * m)), (u >> 3) * 32 + r32);
+            const bool sees = (bits >> (u & 7)) & 1, mine = half == (u >> 3);
+            const uint32_t word = u & 1 ? 0xffff0000u : 0xffffu;
+            pu32x4 only;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) only[w] = mine && ((u & 7) >> 1) == w ? word : 0u;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+              pf32x16 o;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = 0.f;
+              o = T::mfma32(vf[d] & only, pf & only, o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[d][i] += sees ? o[i] : 0.f;
+            }
+          }
+        }
+      }
+    }
+    lds_barrier();   // before LDS is written again
+  };
+  pass(std::false_type());
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bad |= !(fabsf(acc[d][i]) < INFINITY);
+  if (threadIdx.x == 0) shared_rows[0] = 0;
+  __syncthreads();
+  if (__any(bad && live) && lane == 0) shared_rows[0] = 1;
+  __syncthreads();
+  const bool again = shared_rows[0] != 0;
+  __syncthreads();
+  if (again) pass(std::true_type());   // uniform over the workgroup
+
+  const float l = l_run + __shfl_xor(l_run, 32);
+  any |= __shfl_xor((int)any, 32) != 0;
+  // [unit][virtual row][DH + 4]: maximum, sum, whether a slot was seen, the number of parts, output
+  float* to = work + ((int64_t)blockIdx.x * kPreRows + wv * 32 + r32) * (DH + 4);
+  if (parts > 1 && half == 0) *(pf32x4*)to = pf32x4{m_run, l, any ? 1.f : 0.f, (float)n_parts};
+  if (n_parts == 1) {
+    if (!live) return;
+    uint16_t* o = a.out + row * a.out_stride + h * DH + 4 * half;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = any ? acc[d][i + k] * inv : 0.f;
+        *(pu32x2*)(o + 32 * d + 2 * i) = pu32x2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
+      }
+  } else {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(pf32x4*)(to + 4 + 32 * d + 2 * i + 4 * half) = pf32x4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+  }
+}
+
+// Joins the parts of a split call: DH / 4 threads to a virtual row.
+template <class T, int DH>
+__global__ __launch_bounds__(256) void k_paged_join_rows(const PagedAttnArgs a, const float* work, int parts) {
+  constexpr int RT = DH / 4, R = 256 / RT;   // threads of a row, rows of a workgroup
+  const PagedPool& p = a.pool;
+  const int lane = threadIdx.x & 63;
+  const int G = p.H / p.Hk, per_tile = kPreRows / R;
+  const int piece = blockIdx.x % per_tile, kvh = blockIdx.x / per_tile % p.Hk, number = blockIdx.x / per_tile / p.Hk;
+  const RowTile rt = find_tile(a, G, number, lane);
+  if (rt.seq < 0) return;
+  const int r = piece * R + threadIdx.x / RT, d = threadIdx.x % RT * 4;
+  const int v = rt.first + r;
+  if (v >= rt.rows) return;
+  const float* from = work + (((int64_t)number * parts * p.Hk + kvh) * kPreRows + r) * (DH + 4);
+  const int64_t step = (int64_t)p.Hk * kPreRows * (DH + 4);
+  const int n = (int)from[3];
+  if (n == 1) return;   // part 0 has written the output (a call of several parts writes the number for every tile)
+  float m = -INFINITY;
+  for (int c = 0; c < n; ++c) m = fmaxf(m, from[c * step]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, saw = 0.f;
+  pf32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int c = 0; c < n; ++c) {
+    const pf32x4 x = *(const pf32x4*)(from + c * step);
+    const float f = __builtin_amdgcn_exp2f(x[0] - ref);
+    l += x[1] * f;
+    saw += x[2];
+    o += *(const pf32x4*)(from + c * step + 4 + d) * f;
+  }
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
+  *(pu32x2*)(a.out + (rt.begin + v / G) * a.out_stride + (kvh * G + v % G) * DH + d) =
+      pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+}
+
+PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
+  const int64_t G = p.H / p.Hk, slots = (int64_t)p.max_pages << p.page_shift;
+  const int64_t partial = p.n_seqs < n_rows ? p.n_seqs : n_rows;   // tiles that are not full, at most
+  PagedSplit s{};
+  s.tiles = (n_rows * G) / kPreRows + partial;
+  s.parts = 1;
+  const int64_t base = s.tiles * p.Hk, most = (slots + kPreKeys * kPreMinTiles - 1) / (kPreKeys * kPreMinTiles);
+  if (base > 0 && base < kPreUnits) {
+    const int64_t want = (2 * kPreUnits + base - 1) / base;
+    s.parts = (int)(want < most ? want : most);
+  }
+  s.split = s.parts > 1;
+  s.units = base * s.parts;
+  s.bytes = s.split ? (size_t)s.units * kPreRows * (p.dh + 4) * sizeof(float) : 0;
+  return s;
+}
+
+template <class T, int DH>
+static hipError_t prefill(const PagedAttnArgs& a, const PagedSplit& sp, void* workspace, hipStream_t s) {
+  k_paged_prefill<T, DH><<<(unsigned)sp.units, kPreWaves * 64, 0, s>>>(a, (float*)workspace, sp.parts);
+  if (sp.split)
+    k_paged_join_rows<T, DH><<<(unsigned)(sp.tiles * a.pool.Hk * (kPreRows * DH / 1024)), 256, 0, s>>>(
+        a, (const float*)workspace, sp.parts);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_prefill(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s) {
+  if (dtype == GVC_BF16)
+    return a.pool.dh == 64 ? prefill<Bf16, 64>(a, sp, workspace, s) : prefill<Bf16, 128>(a, sp, workspace, s);
+  return a.pool.dh == 64 ? prefill<Fp16, 64>(a, sp, workspace, s) : prefill<Fp16, 128>(a, sp, workspace, s);
+}
+
+}  // namespace gvc
