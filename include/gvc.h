@@ -418,10 +418,12 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
                          const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,
                          const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream);
 
-/* Device bytes of workspace that gvc_paged_decode (n_rows = n_seqs) or
- * gvc_paged_prefill with n_rows rows needs: partial results where the slots of
- * a row are split over workgroups.  Errors: GVC_EINVAL. */
-int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, size_t* bytes);
+/* Device bytes of workspace that gvc_paged_decode (prefill 0, n_rows ignored)
+ * or gvc_paged_prefill with n_rows rows (prefill 1) needs with this window and
+ * n_sinks: partial results where the slots of a row are split over workgroups.
+ * What the workspace holds before a call does not matter.  Errors: GVC_EINVAL. */
+int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
+                            int32_t n_sinks, size_t* bytes);
 
 /* Attention of one token per sequence: row s of q sees the first lengths[s]
  * slots of sequence s (dev int32 [n_seqs]; 0 or less: none, an idle slot of the

@@ -55,8 +55,11 @@ struct PagedSplit {
   int parts;
   size_t bytes;
 };
-PagedSplit paged_decode_split(const PagedPool& p, int window, int n_sinks);
+// rows: lists of rows, else one row per sequence.
+PagedSplit paged_decode_split(const PagedPool& p, int n_rows, bool rows, int window, int n_sinks);
 PagedSplit paged_prefill_split(const PagedPool& p, int n_rows);
+// Whether a call with lists of rows goes to the decode kernel.
+bool paged_few_rows(const PagedPool& p, int n_rows, int window, int n_sinks);
 
 hipError_t launch_paged_decode(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s);
 hipError_t launch_paged_prefill(const PagedAttnArgs& a, const PagedSplit& sp, int dtype, void* workspace, hipStream_t s);

@@ -63,19 +63,43 @@ const char* bad_rows(const void* p, int64_t stride, int heads, int dh, int n_row
   return nullptr;
 }
 
+const char* bad_reach(int32_t window, int32_t n_sinks) noexcept {
+  return window < 0 || n_sinks < 0 ? "window and n_sinks must be >= 0" : nullptr;
+}
+
+const char* bad_row_count(const gvc_paged_desc& d, int32_t n_rows) noexcept {
+  return n_rows < 0 || (int64_t)n_rows * d.n_heads >= kMaxHeadRows ? "n_rows must be >= 0, and n_rows * n_heads below 2^28"
+                                                                   : nullptr;
+}
+
+// A window over every slot hides none.
+struct Reach {
+  int window, sinks;
+};
+Reach reach(const gvc_paged_desc& d, int32_t window, int32_t n_sinks) noexcept {
+  const int slots = d.max_pages * d.page_size;
+  return {window >= slots ? 0 : window, std::min(n_sinks, slots)};
+}
+
+// The kernel that a call takes (tiled: the prefill kernel) and how it is cut.
+PagedSplit plan(const PagedPool& p, int n_rows, bool lists, const Reach& r, bool& tiled) noexcept {
+  tiled = lists && !paged_few_rows(p, n_rows, r.window, r.sinks);
+  return tiled ? paged_prefill_split(p, n_rows) : paged_decode_split(p, n_rows, lists, r.window, r.sinks);
+}
+
 int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
                int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows, const void* k_pages,
                const void* v_pages, const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
                size_t workspace_bytes, void* stream) noexcept {
   const gvc_paged_desc& d = *desc;
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail("scale must be positive and finite");
-  if (window < 0 || n_sinks < 0) return fail("window and n_sinks must be >= 0");
+  if (const char* w = bad_reach(window, n_sinks)) return fail(w);
   if (n_rows == 0) return GVC_OK;
   if (!row_last || !k_pages || !v_pages || !page_table) return fail("null argument");
   if (!aligned(k_pages) || !aligned(v_pages)) return fail("pages must be 16-byte aligned");
   if (const char* w = bad_rows(q, q_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
   if (const char* w = bad_rows(out, out_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
-  const int64_t slots = (int64_t)d.max_pages * d.page_size;
+  const Reach seen = reach(d, window, n_sinks);
   PagedAttnArgs a{};
   a.pool = pool_of(d, k_pages, v_pages, page_table);
   a.q = static_cast<const uint16_t*>(q);
@@ -85,15 +109,16 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.row_last = row_last;
   a.row_begin = row_begin;
   a.n_rows = n_rows;
-  a.window = window >= slots ? 0 : window;   // a window over every slot hides none
-  a.n_sinks = (int)std::min<int64_t>(n_sinks, slots);
+  a.window = seen.window;
+  a.n_sinks = seen.sinks;
   a.scale_log2e = scale * 1.44269504088896340736f;
-  const PagedSplit sp = row_begin ? paged_prefill_split(a.pool, n_rows) : paged_decode_split(a.pool, a.window, a.n_sinks);
+  bool tiled;
+  const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, tiled);
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))
     return set_error(GVC_ENOMEM, "the workspace is too small (or not 16-byte aligned)");
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return device(row_begin ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
-                          : launch_paged_decode(a, sp, d.dtype, workspace, s));
+  return device(tiled ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
+                      : launch_paged_decode(a, sp, d.dtype, workspace, s));
 }
 
 }  // namespace
@@ -157,11 +182,15 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   return device(launch_paged_append(a, d.dtype, static_cast<hipStream_t>(stream)));
 }
 
-int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, size_t* bytes) {
+int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
+                            int32_t n_sinks, size_t* bytes) {
   if (const char* w = bad_desc(desc)) return fail(w);
-  if (!bytes || n_rows < 0) return fail("null bytes or negative n_rows");
-  const PagedPool p = pool_of(*desc, nullptr, nullptr, nullptr);
-  *bytes = prefill ? paged_prefill_split(p, n_rows).bytes : paged_decode_split(p, 0, 0).bytes;
+  if (const char* w = bad_reach(window, n_sinks)) return fail(w);
+  if (!bytes) return fail("null bytes");
+  if (prefill && bad_row_count(*desc, n_rows)) return fail(bad_row_count(*desc, n_rows));
+  bool tiled;
+  *bytes = plan(pool_of(*desc, nullptr, nullptr, nullptr), prefill ? n_rows : desc->n_seqs, prefill != 0,
+                reach(*desc, window, n_sinks), tiled).bytes;
   return GVC_OK;
 }
 
@@ -179,8 +208,7 @@ int32_t gvc_paged_prefill(const gvc_paged_desc* desc, float scale, int32_t windo
                           const void* k_pages, const void* v_pages, const int32_t* page_table, void* out,
                           int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
   if (const char* w = bad_desc(desc)) return fail(w);
-  if (n_rows < 0 || (int64_t)n_rows * desc->n_heads >= kMaxHeadRows)
-    return fail("n_rows must be >= 0, and n_rows * n_heads below 2^28");
+  if (const char* w = bad_row_count(*desc, n_rows)) return fail(w);
   if (n_rows && !row_begin) return fail("null argument");
   return attend(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages, v_pages, page_table,
                 out, out_stride, workspace, workspace_bytes, stream);

@@ -15,7 +15,7 @@
 // workgroups take different key-value heads, so an XCD's L2 holds the keys and
 // values of few heads.  Few rows over many slots are split over the slots as
 // well; a second launch joins the parts.
-#include "gvc_paged.h"
+#include "gvc_paged_rows.h"
 #include "gvc_sync.h"
 
 #define GPA(p) ((const void __attribute__((address_space(1)))*)(p))
@@ -24,51 +24,35 @@
 namespace gvc {
 
 constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves, kPreKeys = 64;
-constexpr int kPreUnits = 512;   // calls with fewer units split the slots, into about twice as many
+constexpr int kPreUnits = 512;   // calls with fewer units split the slots, into about as many
 constexpr int kPreMinTiles = 4;  // tiles of a part, at least
-
-__device__ __forceinline__ int uniform32(int v) { return __builtin_amdgcn_readfirstlane(v); }
+constexpr int kPreMaxParts = kPreUnits;
 
 // The tile of virtual rows that a workgroup takes.
 struct RowTile {
   int seq, first, begin, rows;   // sequence (-1: none), the tile's first virtual row, the sequence's first row, its virtual rows
 };
 
-__device__ __forceinline__ int rows_of(const PagedAttnArgs& a, int s, int& begin) {
-  begin = min(max(a.row_begin[s], 0), a.n_rows);
-  return max(min(a.row_begin[s + 1], a.n_rows) - begin, 0);
-}
-
-__device__ __forceinline__ int scan64(int v, int lane) {   // inclusive
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(v, m);
-    if (lane >= m) v += o;
-  }
-  return v;
-}
-
 // Tile `number` of the call, counted from the last sequence's last rows.
 __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs& a, int G, int number, int lane) {
   RowTile t{-1, 0, 0, 0};
   for (int s1 = a.pool.n_seqs; s1 > 0; s1 -= 64) {
     const int s = s1 - 1 - lane;
-    int begin = 0;
-    const int rows = s >= 0 ? rows_of(a, s, begin) * G : 0;
-    const int n = (rows + kPreRows - 1) / kPreRows;
-    const int sum = scan64(n, lane);
+    const SeqRows r = seq_rows<true>(a, max(s, 0), G);
+    const int n = s >= 0 ? (r.rows + kPreRows - 1) / kPreRows : 0;
+    const int sum = wave_scan(n);
     const uint64_t past = __ballot(sum > number);
     if (past) {
       const int l = __builtin_ctzll(past);
       t.seq = s1 - 1 - l;
-      t.begin = __builtin_amdgcn_readlane(begin, l);
-      t.rows = __builtin_amdgcn_readlane(rows, l);
+      t.begin = __builtin_amdgcn_readlane(r.begin, l);
+      t.rows = __builtin_amdgcn_readlane(r.rows, l);
       t.first = (__builtin_amdgcn_readlane(sum, l) - 1 - number) * kPreRows;
       break;
     }
     number -= __builtin_amdgcn_readlane(sum, 63);
   }
-  return {uniform32(t.seq), uniform32(t.first), uniform32(t.begin), uniform32(t.rows)};
+  return {uniform(t.seq), uniform(t.first), uniform(t.begin), uniform(t.rows)};
 }
 
 template <class T, int DH>
@@ -80,7 +64,7 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
   constexpr int kTile = kPreKeys * DH * 2; // bytes of K, and of V
   __shared__ __attribute__((aligned(16))) char lds[2][2][kTile];
   const PagedPool& p = a.pool;
-  const int lane = threadIdx.x & 63, wv = uniform32(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   const int r32 = lane & 31, half = lane >> 5;
   const int G = p.H / p.Hk, kvh = blockIdx.x % p.Hk, part = blockIdx.x / p.Hk % parts;
   const RowTile rt = find_tile(a, G, blockIdx.x / p.Hk / parts, lane);
@@ -112,12 +96,12 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
     lo = min(lo, shared_rows[kPreWaves + w]);
   }
   __syncthreads();
-  hi = uniform32(hi);
-  lo = uniform32(lo);
-  const int lo_all = uniform32(a.window ? hi_some - a.window : -1);
-  hi_some = uniform32(hi_some);
-  hi_all = uniform32(hi_all);
-  lo_some = uniform32(a.window ? lo_some - a.window : -1);
+  hi = uniform(hi);
+  lo = uniform(lo);
+  const int lo_all = uniform(a.window ? hi_some - a.window : -1);
+  hi_some = uniform(hi_some);
+  hi_all = uniform(hi_all);
+  lo_some = uniform(a.window ? lo_some - a.window : -1);
   const int lo_row = a.window ? last - a.window : -1;
   // the workgroup's tiles: the sinks', then the window's; and this part of them
   const int end = (hi >> 6) + 1, win_lo = a.window ? max(lo - a.window + 1, 0) >> 6 : 0;
@@ -175,37 +159,131 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
   for (int m = 0; m < 4; ++m) v_at[m] = kTile + r32 * 128 + (((2 * m + half) ^ (r32 & 7)) << 4);
 
   pf32x16 acc[ND];
-  float m_run, l_run;   // maximum (powers of two), this lane's share of the sum
-  bool any;
-  // CAREFUL: values in slots that only some rows of the wave see are added slot
-  // by slot, so that NaN and infinities there stay with the rows that see them.
-  auto pass = [&](auto careful) {
+  float m_run = -INFINITY, l_run = 0.f;   // maximum (powers of two), this lane's share of the sum
+  bool any = false;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  float shift = T::kShift;   // a score's exponent is score * scale + shift
+  int next_id = 0;
+  uint64_t ok = 0;
+  if (t_begin < t_end) {
+    const int id = load_ids(t_begin);
+    next_id = load_ids(t_begin + 1);
+    copy(t_begin, id);
+    ok = __ballot((unsigned)id < (unsigned)p.n_pages);
+  }
+  for (int t = t_begin; t < t_end; ++t) {
+    wait_vmcnt<0>();   // this wave's copies of tile t
+    lds_barrier();     // everyone's, and everyone is done with tile t - 1
+    uint64_t next_ok = 0;
+    if (t + 1 < t_end) {
+      copy(t + 1, next_id);
+      next_ok = __ballot((unsigned)next_id < (unsigned)p.n_pages);
+      next_id = load_ids(t + 2);
+    }
+    const int j0 = tile_slot(t);
+    const unsigned pages = (unsigned)ok & 0xff;   // of the tile's chunks
+    ok = next_ok;
+    if (j0 > hi_some || (j0 + 63 <= lo_some && j0 >= a.n_sinks)) continue;   // nothing for this wave
+    const bool full = pages == 0xff && j0 + 63 <= hi_all && j0 > lo_all;
+    const char* st = lds[t & 1][0];
+    pf32x16 s[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[e][i] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk)
+        s[e] = T::mfma32(*(const pu32x4*)(st + k_at[kk] + e * 32 * CR * 16), qf[kk], s[e]);
+    }
+    uint32_t seen = ~0u, some = ~0u;   // element 16 e + i is slot j0 + 32 e + 16 (i / 8) + 8 half + i % 8
+    if (!full) {
+      seen = some = 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int c = 2 * (i >> 3) + half, j = j0 + 8 * c + (i & 7);
+        const bool on = (pages >> c) & 1;
+        const bool in = on & (j <= last) & ((j > lo_row) | (j < a.n_sinks));
+        const bool by = on & (j <= hi_some) & ((j > lo_some) | (j < a.n_sinks));
+        s[i >> 4][i & 15] = in ? s[i >> 4][i & 15] : -INFINITY;
+        seen |= (uint32_t)in << i;
+        some |= (uint32_t)by << i;
+      }
+    }
+    any |= seen != 0;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+    top *= a.scale_log2e;   // positive
+    if (__any(top > m_run + kPagedLazy)) {
+      const float mn = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32))), nb = mn == -INFINITY ? 0.f : mn;
+      const float f = __builtin_amdgcn_exp2f(m_run - nb);
+      m_run = mn;
+      shift = T::kShift - nb;
+      l_run *= f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] *= f;
+    }
+    float x[32], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, shift));
+      sum += x[i];
+    }
+    l_run += sum;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float* y = x + 8 * m;
+      const pu32x4 pf = {pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
+      pu32x4 vf[ND];
+#pragma unroll
+      for (int d = 0; d < ND; ++d) vf[d] = *(const pu32x4*)(st + v_at[m] + d * 32 * 128);
+      if (!full) {   // values that no row of the wave sees become zeros (0 x NaN is NaN)
+        const uint32_t b = some >> (8 * m);
+        pu32x4 keep;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          keep[w] = ((b >> (2 * w)) & 1 ? 0xffffu : 0u) | ((b >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) vf[d] &= keep;
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] = T::mfma32(vf[d], pf, acc[d]);
+    }
+  }
+  // Where an output is not finite the workgroup does its rows again, slowly: a
+  // slot that only some rows of a wave see is added to those alone, so that NaN
+  // and infinities in its values stay with them.
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bad |= !(fabsf(acc[d][i]) < INFINITY);
+  const int wave_bad = __any(bad && live);
+  __syncthreads();   // LDS is free
+  if (lane == 0) shared_rows[wv] = wave_bad;
+  __syncthreads();
+  bool again = false;
+#pragma unroll
+  for (int w = 0; w < kPreWaves; ++w) again |= shared_rows[w] != 0;
+  __syncthreads();
+  if (again) {
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
     m_run = -INFINITY;
     l_run = 0.f;
-    any = false;
-    float shift = T::kShift;   // a score's exponent is score * scale + shift
-    if (t_begin >= t_end) return;
-    int id = load_ids(t_begin), next_id = load_ids(t_begin + 1);
-    copy(t_begin, id);
-    uint64_t ok = __ballot((unsigned)id < (unsigned)p.n_pages);
+#pragma unroll 1
     for (int t = t_begin; t < t_end; ++t) {
-      wait_vmcnt<0>();   // this wave's copies of tile t
-      lds_barrier();     // everyone's, and everyone is done with tile t - 1
-      uint64_t next_ok = 0;
-      if (t + 1 < t_end) {
-        copy(t + 1, next_id);
-        next_ok = __ballot((unsigned)next_id < (unsigned)p.n_pages);
-        next_id = load_ids(t + 2);
-      }
+      const int id = load_ids(t);
+      copy(t, id);
+      const unsigned pages = (unsigned)__ballot((unsigned)id < (unsigned)p.n_pages) & 0xff;
+      wait_vmcnt<0>();
+      __syncthreads();
       const int j0 = tile_slot(t);
-      const unsigned pages = (unsigned)ok & 0xff;   // of the tile's chunks
-      ok = next_ok;
-      if (j0 > hi_some || (j0 + 63 <= lo_some && j0 >= a.n_sinks)) continue;   // nothing for this wave
-      const bool full = pages == 0xff && j0 + 63 <= hi_all && j0 > lo_all;
       const char* st = lds[t & 1][0];
       pf32x16 s[2];
 #pragma unroll
@@ -216,95 +294,46 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
         for (int kk = 0; kk < NK; ++kk)
           s[e] = T::mfma32(*(const pu32x4*)(st + k_at[kk] + e * 32 * CR * 16), qf[kk], s[e]);
       }
-      uint32_t seen = ~0u, some = ~0u;   // element 16 e + i is slot j0 + 32 e + 16 (i / 8) + 8 half + i % 8
-      if (!full) {
-        seen = some = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int c = 2 * (i >> 3) + half, j = j0 + 8 * c + (i & 7);
-          const bool on = (pages >> c) & 1;
-          const bool in = on & (j <= last) & ((j > lo_row) | (j < a.n_sinks));
-          const bool by = on & (j <= hi_some) & ((j > lo_some) | (j < a.n_sinks));
-          s[i >> 4][i & 15] = in ? s[i >> 4][i & 15] : -INFINITY;
-          seen |= (uint32_t)in << i;
-          some |= (uint32_t)by << i;
-        }
-      }
-      any |= seen != 0;
+      uint32_t seen = 0;
       float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-      top *= a.scale_log2e;   // positive
-      if (__any(top > m_run + kPagedLazy)) {
-        const float mn = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32))), nb = mn == -INFINITY ? 0.f : mn;
-        const float f = __builtin_amdgcn_exp2f(m_run - nb);
-        m_run = mn;
-        shift = T::kShift - nb;
-        l_run *= f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) acc[d] *= f;
-      }
-      float x[32];
-#pragma unroll
       for (int i = 0; i < 32; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, shift));
-        l_run += x[i];
+        const int c = 2 * (i >> 3) + half, j = j0 + 8 * c + (i & 7);
+        const bool in = ((pages >> c) & 1) & (j <= last) & ((j > lo_row) | (j < a.n_sinks));
+        s[i >> 4][i & 15] = in ? s[i >> 4][i & 15] : -INFINITY;
+        seen |= (uint32_t)in << i;
+        top = fmaxf(top, s[i >> 4][i & 15]);
       }
+      const float mn = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2e), nb = mn == -INFINITY ? 0.f : mn;
+      const float f = __builtin_amdgcn_exp2f(m_run - nb);
+      m_run = mn;
+      l_run *= f;
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float* y = x + 8 * m;
-        const pu32x4 pf = {pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
-        pu32x4 vf[ND];
+      for (int d = 0; d < ND; ++d) acc[d] *= f;
 #pragma unroll
-        for (int d = 0; d < ND; ++d) vf[d] = *(const pu32x4*)(st + v_at[m] + d * 32 * 128);
-        if (!full) {   // values that no row of the wave sees become zeros (0 x NaN is NaN)
-          const uint32_t b = some >> (8 * m);
-          pu32x4 keep;
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            keep[w] = ((b >> (2 * w)) & 1 ? 0xffffu : 0u) | ((b >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+        for (int j = 0; j < 8; ++j) {
+          const int i = 8 * m + j;
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, T::kShift - nb));
+          l_run += x;
+#pragma unroll 1
+          for (int o = 0; o < 2; ++o) {   // slot 16 m + 8 o + j, of the lanes with half == o
+            const float pr = T::up((uint16_t)pack2<T>(__shfl(x, 32 * o + r32), 0.f));
+            if (!(((unsigned)__shfl((int)seen, 32 * o + r32) >> i) & 1)) continue;
 #pragma unroll
-          for (int d = 0; d < ND; ++d) vf[d] &= keep;
-        }
-        if (!decltype(careful)::value || full) {
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int d = 0; d < ND; ++d) acc[d] = T::mfma32(vf[d], pf, acc[d]);
-        } else {
-          for (int u = 0; u < 16; ++u) {   // slot 16 m + u of the tile: element u % 8 of the lanes with half == u / 8
-            const unsigned bits = (unsigned)__shfl((int)(seen >> (8 * m)), (u >> 3) * 32 + r32);
-            const bool sees = (bits >> (u & 7)) & 1, mine = half == (u >> 3);
-            const uint32_t word = u & 1 ? 0xffff0000u : 0xffffu;
-            pu32x4 only;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) only[w] = mine && ((u & 7) >> 1) == w ? word : 0u;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              pf32x16 o;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = 0.f;
-              o = T::mfma32(vf[d] & only, pf & only, o);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[d][i] += sees ? o[i] : 0.f;
-            }
+              for (int k = 0; k < 16; ++k) {
+                const int dim = 32 * d + 8 * (k >> 2) + 4 * half + (k & 3);
+                const char* vp = st + kTile + dim * 128 + (((2 * m + o) ^ (dim & 7)) << 4) + 2 * j;
+                acc[d][k] = fmaf(pr, T::up(*(const uint16_t*)vp), acc[d][k]);
+              }
           }
         }
-      }
+      __syncthreads();
     }
-    lds_barrier();   // before LDS is written again
-  };
-  pass(std::false_type());
-  bool bad = false;
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) bad |= !(fabsf(acc[d][i]) < INFINITY);
-  if (threadIdx.x == 0) shared_rows[0] = 0;
-  __syncthreads();
-  if (__any(bad && live) && lane == 0) shared_rows[0] = 1;
-  __syncthreads();
-  const bool again = shared_rows[0] != 0;
-  __syncthreads();
-  if (again) pass(std::true_type());   // uniform over the workgroup
+  }
 
   const float l = l_run + __shfl_xor(l_run, 32);
   any |= __shfl_xor((int)any, 32) != 0;
@@ -333,41 +362,47 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
   }
 }
 
-// Joins the parts of a split call: DH / 4 threads to a virtual row.
-template <class T, int DH>
-__global__ __launch_bounds__(256) void k_paged_join_rows(const PagedAttnArgs a, const float* work, int parts) {
-  constexpr int RT = DH / 4, R = 256 / RT;   // threads of a row, rows of a workgroup
+// Joins the parts of a split call.  RT threads to a row and head: a whole
+// workgroup where there are many parts, else DH / 4.
+template <class T, int DH, bool MANY>
+__global__ __launch_bounds__(256) void k_paged_join_tiles(const PagedAttnArgs a, const float* work, int parts) {
+  constexpr int RT = MANY ? 256 : DH / 4, R = 256 / RT;
   const PagedPool& p = a.pool;
-  const int lane = threadIdx.x & 63;
-  const int G = p.H / p.Hk, per_tile = kPreRows / R;
+  const int lane = threadIdx.x & 63, G = p.H / p.Hk;
+  const int per_tile = kPreRows / R;
   const int piece = blockIdx.x % per_tile, kvh = blockIdx.x / per_tile % p.Hk, number = blockIdx.x / per_tile / p.Hk;
   const RowTile rt = find_tile(a, G, number, lane);
-  if (rt.seq < 0) return;
-  const int r = piece * R + threadIdx.x / RT, d = threadIdx.x % RT * 4;
-  const int v = rt.first + r;
-  if (v >= rt.rows) return;
+  const int r = piece * R + threadIdx.x / RT, v = rt.first + r;
+  if (rt.seq < 0 || v >= rt.rows) return;   // MANY: uniform
   const float* from = work + (((int64_t)number * parts * p.Hk + kvh) * kPreRows + r) * (DH + 4);
   const int64_t step = (int64_t)p.Hk * kPreRows * (DH + 4);
-  const int n = (int)from[3];
-  if (n == 1) return;   // part 0 has written the output (a call of several parts writes the number for every tile)
-  float m = -INFINITY;
-  for (int c = 0; c < n; ++c) m = fmaxf(m, from[c * step]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f, saw = 0.f;
-  pf32x4 o = {0, 0, 0, 0};
+  const int n = (int)from[3];   // written for every row of a call of several parts
+  if (n == 1) return;           // part 0 has written the output
+  uint16_t* out = a.out + (rt.begin + v / G) * a.out_stride + (kvh * G + v % G) * DH;
+  if constexpr (MANY) {
+    __shared__ JoinLds<DH, 256, kPreMaxParts> lds;
+    join_row<T, DH, 256>(from, step, n, lds, out);
+  } else {
+    const int d = threadIdx.x % RT * 4;
+    float m = -INFINITY;
 #pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const pf32x4 x = *(const pf32x4*)(from + c * step);
-    const float f = __builtin_amdgcn_exp2f(x[0] - ref);
-    l += x[1] * f;
-    saw += x[2];
-    o += *(const pf32x4*)(from + c * step + 4 + d) * f;
-  }
-  const float inv = 1.f / l;
+    for (int c = 0; c < n; ++c) m = fmaxf(m, from[c * step]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, saw = 0.f;
+    pf32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int c = 0; c < n; ++c) {
+      const pf32x4 x = *(const pf32x4*)(from + c * step);
+      const float f = __builtin_amdgcn_exp2f(x[0] - ref);
+      l += x[1] * f;
+      saw += x[2];
+      o += *(const pf32x4*)(from + c * step + 4 + d) * f;
+    }
+    const float inv = 1.f / l;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-  *(pu32x2*)(a.out + (rt.begin + v / G) * a.out_stride + (kvh * G + v % G) * DH + d) =
-      pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+    for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
+    *(pu32x2*)(out + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+  }
 }
 
 PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
@@ -377,8 +412,8 @@ PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
   s.tiles = (n_rows * G) / kPreRows + partial;
   s.parts = 1;
   const int64_t base = s.tiles * p.Hk, most = (slots + kPreKeys * kPreMinTiles - 1) / (kPreKeys * kPreMinTiles);
-  if (base > 0 && base < kPreUnits) {
-    const int64_t want = (2 * kPreUnits + base - 1) / base;
+  if (base > 0 && base <= kPreUnits / 2) {
+    const int64_t want = kPreUnits / base;
     s.parts = (int)(want < most ? want : most);
   }
   s.split = s.parts > 1;
@@ -390,9 +425,11 @@ PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
 template <class T, int DH>
 static hipError_t prefill(const PagedAttnArgs& a, const PagedSplit& sp, void* workspace, hipStream_t s) {
   k_paged_prefill<T, DH><<<(unsigned)sp.units, kPreWaves * 64, 0, s>>>(a, (float*)workspace, sp.parts);
-  if (sp.split)
-    k_paged_join_rows<T, DH><<<(unsigned)(sp.tiles * a.pool.Hk * (kPreRows * DH / 1024)), 256, 0, s>>>(
-        a, (const float*)workspace, sp.parts);
+  if (sp.split) {
+    const unsigned rows = (unsigned)(sp.tiles * a.pool.Hk * kPreRows);
+    if (sp.parts > 16) k_paged_join_tiles<T, DH, true><<<rows, 256, 0, s>>>(a, (const float*)workspace, sp.parts);
+    else k_paged_join_tiles<T, DH, false><<<rows * (DH / 4) / 256, 256, 0, s>>>(a, (const float*)workspace, sp.parts);
+  }
   return hipGetLastError();
 }
 

@@ -112,7 +112,7 @@ def lib():
         pd, f32, i64 = ctypes.POINTER(PagedDesc), ctypes.c_float, ctypes.c_int64
         L.gvc_paged_append.argtypes = [pd, ctypes.POINTER(PagedRope), vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp,
                                        vp, i64, vp]
-        L.gvc_paged_workspace.argtypes = [pd, i32, i32, ctypes.POINTER(sz)]
+        L.gvc_paged_workspace.argtypes = [pd, i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.gvc_paged_decode.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, sz, vp]
         L.gvc_paged_prefill.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, sz, vp]
         L.gvc_paged_check.argtypes = [pd, vp, vp, vp, vp, i32]
@@ -224,9 +224,9 @@ def paged_append(desc: PagedDesc, rope: PagedRope, q, q_stride: int, k: int, k_s
                                   v_pages, page_table, q_out, q_out_stride, stream))
 
 
-def paged_workspace(desc: PagedDesc, prefill: bool, n_rows: int) -> int:
+def paged_workspace(desc: PagedDesc, prefill: bool, n_rows: int, window: int = 0, n_sinks: int = 0) -> int:
     n = ctypes.c_size_t()
-    _check(lib().gvc_paged_workspace(desc, int(prefill), n_rows, ctypes.byref(n)))
+    _check(lib().gvc_paged_workspace(desc, int(prefill), n_rows, window, n_sinks, ctypes.byref(n)))
     return n.value
 
 

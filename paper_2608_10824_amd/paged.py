@@ -106,7 +106,7 @@ class PagedCache:
         _need(n == self.n_seqs, "q must have one row per sequence")
         self._ints(lengths, "lengths", n)
         desc = self._with(heads)
-        work = self._workspace(desc, False, n)
+        work = self._workspace(desc, False, n, window, sinks)
         self._call(gvc.paged_decode, desc, self._scale(scale), window, sinks, q.data_ptr(), qs, lengths.data_ptr(),
                    *self._pages, out.data_ptr(), os,
                    *_address(work))
@@ -121,7 +121,7 @@ class PagedCache:
         self._ints(row_last, "row_last", n)
         self._ints(row_begin, "row_begin", self.n_seqs + 1)
         desc = self._with(heads)
-        work = self._workspace(desc, True, n)
+        work = self._workspace(desc, True, n, window, sinks)
         self._call(gvc.paged_prefill, desc, self._scale(scale), window, sinks, q.data_ptr(), qs, row_last.data_ptr(),
                    row_begin.data_ptr(), n, *self._pages, out.data_ptr(), os,
                    *_address(work))
@@ -181,10 +181,10 @@ class PagedCache:
     def _scale(self, scale):
         return self.head_dim ** -0.5 if scale is None else scale
 
-    def _workspace(self, desc, prefill, n):
+    def _workspace(self, desc, prefill, n, window, sinks):
         """Workspace for one call (None: none needed), from the caching
         allocator: it is this call's alone on any stream and in any graph."""
-        size = gvc.paged_workspace(desc, prefill, n)
+        size = gvc.paged_workspace(desc, prefill, n, window, sinks)
         return torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
 
     def _call(self, f, *args):

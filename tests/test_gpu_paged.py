@@ -366,6 +366,16 @@ def test_prefill_rows_that_see_nothing_and_rows_of_no_sequence():
     pool.expect(out[2:], q[2:], [1] * 3 + [2] * 5, [9] * 8)
 
 
+@pytest.mark.parametrize("rows,length", [(10, 50), (10, 3000), (300, 3000)])
+def test_prefill_with_bounds_that_fall(rows, length):
+    """Bounds have to rise; where they do not, no row outside them is touched (nor any other memory)."""
+    pool = Pool(26, "bf16", 2, 64, 16, [length] * 4)
+    q = pool.rows(rows + 9, 4)
+    held = torch.full((rows + 9, 4, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    pool.cache.prefill(q, pool.ints([length - 1] * (rows + 9)), pool.ints([0, rows, 0, rows, rows + 7]), out=held)
+    assert (held[rows + 7:] == 5).all()
+
+
 def test_values_of_later_slots_do_not_reach_earlier_rows():
     """NaN and infinities in the keys and values of slots that only later rows
     see: earlier rows are finite and right, later ones show them."""
