@@ -216,12 +216,12 @@ def destroy(ctx: int):
     _check(lib().gvc_destroy(ctx))
 
 
-# ---- the paged cache (gvc_paged_*): device addresses as integers, strides in elements
-def paged_append(desc: PagedDesc, rope: PagedRope, q, q_stride: int, k: int, k_stride: int, v: int, v_stride: int,
-                 row_seq: int, row_slot: int, n_rows: int, k_pages: int, v_pages: int, page_table: int, q_out,
-                 q_out_stride: int, stream: int):
-    _check(lib().gvc_paged_append(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows, k_pages,
-                                  v_pages, page_table, q_out, q_out_stride, stream))
+# ---- the paged cache (gvc_paged_*): device addresses as integers (None where
+# the C call takes NULL), row strides in elements, the stream last
+def paged_append(*args):
+    """(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows, k_pages, v_pages, page_table,
+    q_out, q_out_stride, stream)"""
+    _check((_lib or lib()).gvc_paged_append(*args))
 
 
 def paged_workspace(desc: PagedDesc, prefill: bool, n_rows: int, window: int = 0, n_sinks: int = 0) -> int:
@@ -230,18 +230,16 @@ def paged_workspace(desc: PagedDesc, prefill: bool, n_rows: int, window: int = 0
     return n.value
 
 
-def paged_decode(desc: PagedDesc, scale: float, window: int, n_sinks: int, q: int, q_stride: int, lengths: int,
-                 k_pages: int, v_pages: int, page_table: int, out: int, out_stride: int, workspace, workspace_bytes: int,
-                 stream: int):
-    _check(lib().gvc_paged_decode(desc, scale, window, n_sinks, q, q_stride, lengths, k_pages, v_pages, page_table, out,
-                                  out_stride, workspace, workspace_bytes, stream))
+def paged_decode(*args):
+    """(desc, scale, window, n_sinks, q, q_stride, lengths, k_pages, v_pages, page_table, out, out_stride, workspace,
+    workspace_bytes, stream)"""
+    _check((_lib or lib()).gvc_paged_decode(*args))
 
 
-def paged_prefill(desc: PagedDesc, scale: float, window: int, n_sinks: int, q: int, q_stride: int, row_last: int,
-                  row_begin: int, n_rows: int, k_pages: int, v_pages: int, page_table: int, out: int, out_stride: int,
-                  workspace, workspace_bytes: int, stream: int):
-    _check(lib().gvc_paged_prefill(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages,
-                                   v_pages, page_table, out, out_stride, workspace, workspace_bytes, stream))
+def paged_prefill(*args):
+    """(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages, v_pages, page_table, out,
+    out_stride, workspace, workspace_bytes, stream)"""
+    _check((_lib or lib()).gvc_paged_prefill(*args))
 
 
 def paged_check(desc: PagedDesc, page_table: int, lengths, row_seq, row_slot, n_rows: int):

@@ -12,18 +12,25 @@ tensors that require a gradient are refused.
     o = cache.prefill(q, row_slot, row_begin)            # the rows of a prompt
     o = cache.decode(q, lengths, window=4096, sinks=4)   # one new token per sequence
 """
-import ctypes
-
 import torch
 
 from . import gvc
 
 _DTYPES = {torch.bfloat16: gvc.BF16, torch.float16: gvc.FP16}
 
+# Descriptors and workspace sizes by shape: making one costs more than a short
+# call's other checks together.
+_descs, _sizes = {}, {}
+_KEPT = 4096
 
-def _need(ok, text):
-    if not ok:
-        raise ValueError(text)
+
+def _kept(store, key, make):
+    value = store.get(key)
+    if value is None:
+        if len(store) >= _KEPT:
+            store.clear()
+        value = store[key] = make()
+    return value
 
 
 def _address(t):
@@ -37,21 +44,30 @@ class PagedCache:
     tensors stay the caller's: the table may be changed between calls."""
 
     def __init__(self, k_pages, v_pages, page_table):
-        _need(k_pages.dtype in _DTYPES and v_pages.dtype == k_pages.dtype, "pages must be bfloat16 or float16, both alike")
-        _need(k_pages.dim() == 4, "k_pages must be [n_pages][n_kv_heads][page_size][head_dim]")
-        n_pages, kv, page, dh = k_pages.shape
-        _need(v_pages.shape == (n_pages, kv, dh, page), "v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
-        _need(page_table.dtype == torch.int32 and page_table.dim() == 2, "page_table must be int32 [n_seqs][max_pages]")
-        _need(k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous(),
-              "pages and page table must be contiguous")
-        self.device = k_pages.device
-        _need(self.device.type == "cuda" and v_pages.device == self.device and page_table.device == self.device,
-              "pages and page table must be on one GPU")
+        dtype = k_pages.dtype
+        if dtype not in _DTYPES or v_pages.dtype != dtype:
+            raise ValueError("pages must be bfloat16 or float16, both alike")
+        if k_pages.dim() != 4:
+            raise ValueError("k_pages must be [n_pages][n_kv_heads][page_size][head_dim]")
+        n_pages, kv, page, dh = shape = k_pages.shape
+        if v_pages.shape != (n_pages, kv, dh, page):
+            raise ValueError("v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [n_seqs][max_pages]")
+        if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous()):
+            raise ValueError("pages and page table must be contiguous")
+        index = k_pages.get_device()
+        if index < 0 or v_pages.get_device() != index or page_table.get_device() != index:
+            raise ValueError("pages and page table must be on one GPU")
         self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
-        self.n_seqs = page_table.shape[0]
+        self.n_seqs, columns = page_table.shape
         self.n_kv_heads, self.head_dim = kv, dh
-        self._desc = gvc.PagedDesc(_DTYPES[k_pages.dtype], kv, kv, dh, page, n_pages, self.n_seqs, page_table.shape[1])
-        self._pages = (k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr())
+        self._dtype, self._index = dtype, index
+        self._shape = (dtype, *shape, self.n_seqs, columns)
+
+    @property
+    def device(self):
+        return self.k_pages.device
 
     @classmethod
     def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_seqs, max_pages, dtype=torch.bfloat16, device="cuda"):
@@ -68,34 +84,36 @@ class PagedCache:
         rope_pairs: rotated pairs of each axis, at most three (default: the
         whole head on one axis; () rotates nothing); positions: int32
         [axes][rows], default the slots."""
-        n, ks = self._rows(k, "k", self.n_kv_heads)
-        _need(self._rows(v, "v", self.n_kv_heads)[0] == n, "k and v must have the same rows")
+        kv = self.n_kv_heads
+        n, ks = self._rows(k, "k", kv)
+        m, vs = self._rows(v, "v", kv)
+        if m != n:
+            raise ValueError("k and v must have the same rows")
         self._ints(row_seq, "row_seq", n)
         self._ints(row_slot, "row_slot", n)
         pairs = (self.head_dim // 2,) if rope_pairs is None else tuple(rope_pairs)
-        _need(len(pairs) <= 3, "rope_pairs has at most three axes")
-        rope = gvc.PagedRope((ctypes.c_int32 * 3)(*pairs), rope_theta, rms_eps, self._gain(q_norm, "q_norm"),
-                             self._gain(k_norm, "k_norm"))
+        if len(pairs) > 3:
+            raise ValueError("rope_pairs has at most three axes")
+        where = None
         if positions is not None:
-            _need(positions.dtype == torch.int32 and positions.device == self.device and
-                  positions.shape == (len(pairs), n) and positions.is_contiguous(),
-                  "positions must be contiguous int32 [axes][rows]")
-            rope.positions, rope.position_stride = positions.data_ptr(), n
-        heads, qs, os, qp, op = self.n_kv_heads, 0, 0, None, None
+            if (positions.dtype != torch.int32 or positions.get_device() != self._index or
+                    positions.shape != (len(pairs), n) or not positions.is_contiguous()):
+                raise ValueError("positions must be contiguous int32 [axes][rows]")
+            where = positions.data_ptr()
+        rope = gvc.PagedRope(pairs, rope_theta, rms_eps, self._gain(q_norm, "q_norm"), self._gain(k_norm, "k_norm"),
+                             where, n)
         if q is None:
-            _need(q_out is None, "q_out without q")
+            if q_out is not None:
+                raise ValueError("q_out without q")
+            heads, qp, qs, op, os = kv, None, 0, None, 0
         else:
-            heads = q.shape[1] if q.dim() == 3 else 0
-            m, qs = self._rows(q, "q", heads)
-            _need(m == n, "q and k must have the same rows")
-            if q_out is None:
-                q_out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
-            m, os = self._rows(q_out, "q_out", heads)
-            _need(m == n, "q_out must have q's rows")
+            heads, m, qs, q_out, os = self._q_out(q, q_out)
+            if m != n:
+                raise ValueError("q and k must have the same rows")
             qp, op = q.data_ptr(), q_out.data_ptr()
-        kp, vp, table = self._pages
-        self._call(gvc.paged_append, self._with(heads), rope, qp, qs, k.data_ptr(), ks, v.data_ptr(), v.stride(0),
-                   row_seq.data_ptr(), row_slot.data_ptr(), n, kp, vp, table, op, os)
+        self._call(gvc.paged_append, self._desc(heads), rope, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                   row_seq.data_ptr(), row_slot.data_ptr(), n, self.k_pages.data_ptr(), self.v_pages.data_ptr(),
+                   self.page_table.data_ptr(), op, os)
         return q_out
 
     def decode(self, q, lengths, *, scale=None, window=0, sinks=0, out=None):
@@ -103,13 +121,14 @@ class PagedCache:
         row s over the first lengths[s] slots (int32; 0: an idle slot of the
         batch, zeros).  scale: default head_dim^-1/2."""
         heads, n, qs, out, os = self._q_out(q, out)
-        _need(n == self.n_seqs, "q must have one row per sequence")
+        if n != self.n_seqs:
+            raise ValueError("q must have one row per sequence")
         self._ints(lengths, "lengths", n)
-        desc = self._with(heads)
-        work = self._workspace(desc, False, n, window, sinks)
-        self._call(gvc.paged_decode, desc, self._scale(scale), window, sinks, q.data_ptr(), qs, lengths.data_ptr(),
-                   *self._pages, out.data_ptr(), os,
-                   *_address(work))
+        desc = self._desc(heads)
+        work = self._workspace(desc, heads, False, n, window, sinks)
+        self._call(gvc.paged_decode, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks, q.data_ptr(),
+                   qs, lengths.data_ptr(), self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(),
+                   out.data_ptr(), os, *_address(work))
         return out
 
     def prefill(self, q, row_last, row_begin, *, scale=None, window=0, sinks=0, out=None):
@@ -120,11 +139,11 @@ class PagedCache:
         heads, n, qs, out, os = self._q_out(q, out)
         self._ints(row_last, "row_last", n)
         self._ints(row_begin, "row_begin", self.n_seqs + 1)
-        desc = self._with(heads)
-        work = self._workspace(desc, True, n, window, sinks)
-        self._call(gvc.paged_prefill, desc, self._scale(scale), window, sinks, q.data_ptr(), qs, row_last.data_ptr(),
-                   row_begin.data_ptr(), n, *self._pages, out.data_ptr(), os,
-                   *_address(work))
+        desc = self._desc(heads)
+        work = self._workspace(desc, heads, True, n, window, sinks)
+        self._call(gvc.paged_prefill, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks,
+                   q.data_ptr(), qs, row_last.data_ptr(), row_begin.data_ptr(), n, self.k_pages.data_ptr(),
+                   self.v_pages.data_ptr(), self.page_table.data_ptr(), out.data_ptr(), os, *_address(work))
         return out
 
     def check(self, lengths=None, row_seq=None, row_slot=None):
@@ -133,62 +152,69 @@ class PagedCache:
         them to the host: a debugging aid, not for the serving loop."""
         host = [None if t is None else t.to("cpu", torch.int32).contiguous()
                 for t in (self.page_table, lengths, row_seq, row_slot)]
-        _need((row_seq is None) == (row_slot is None), "row_seq and row_slot come together")
-        _need(lengths is None or lengths.numel() == self.n_seqs, "lengths must have one entry per sequence")
-        _need(row_seq is None or row_seq.numel() == row_slot.numel(), "row_seq and row_slot must have the same rows")
-        gvc.paged_check(self._desc, *(None if t is None else t.data_ptr() for t in host),
+        if (row_seq is None) != (row_slot is None):
+            raise ValueError("row_seq and row_slot come together")
+        if lengths is not None and lengths.numel() != self.n_seqs:
+            raise ValueError("lengths must have one entry per sequence")
+        if row_seq is not None and row_seq.numel() != row_slot.numel():
+            raise ValueError("row_seq and row_slot must have the same rows")
+        gvc.paged_check(self._desc(self.n_kv_heads), *(None if t is None else t.data_ptr() for t in host),
                         0 if row_seq is None else row_seq.numel())
 
     # ---- argument checks and marshalling
-    def _with(self, heads):
+    def _desc(self, heads):
         """The descriptor for this many query heads."""
-        d = self._desc
-        if d.n_heads != heads:
-            d = gvc.PagedDesc(d.dtype, heads, d.n_kv_heads, d.head_dim, d.page_size, d.n_pages, d.n_seqs, d.max_pages)
-        return d
+        def make():
+            dtype, n_pages, kv, page, dh, n_seqs, columns = self._shape
+            return gvc.PagedDesc(_DTYPES[dtype], heads, kv, dh, page, n_pages, n_seqs, columns)
+        return _kept(_descs, (self._shape, heads), make)
+
+    def _workspace(self, desc, heads, prefill, n, window, sinks):
+        """Workspace for one call (None: none needed), from the caching
+        allocator: it is this call's alone on any stream and in any graph."""
+        size = _kept(_sizes, (self._shape, heads, prefill, n, window, sinks),
+                     lambda: gvc.paged_workspace(desc, prefill, n, window, sinks))
+        return torch.empty(size, dtype=torch.uint8, device=self.k_pages.device) if size else None
 
     def _rows(self, t, name, heads):
         """(rows, row stride) of t [rows][heads][head_dim]."""
-        if t.dtype != self.k_pages.dtype or t.device != self.device or t.dim() != 3 or t.requires_grad:
+        shape = t.shape
+        if t.dtype != self._dtype or t.get_device() != self._index or len(shape) != 3 or t.requires_grad:
             raise ValueError(name + " must be [rows][heads][head_dim] of the pages' type and device, without gradient")
-        n, h, dh = t.shape
+        n, h, dh = shape
         rs, hs, es = t.stride()
         if h != heads or dh != self.head_dim or h < 1 or (n and (es != 1 or (h > 1 and hs != dh))):
             raise ValueError(name + " must be [rows][heads][head_dim] with dense heads")
         return n, rs if n > 1 else h * dh
 
     def _ints(self, t, name, n):
-        if t.dtype != torch.int32 or t.device != self.device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        if t.dtype != torch.int32 or t.get_device() != self._index or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
             raise ValueError("%s must be a contiguous int32 vector of %d on the cache's GPU" % (name, n))
 
     def _gain(self, t, name):
         if t is None:
             return None
-        if t.dtype != self.k_pages.dtype or t.device != self.device or t.shape != (self.head_dim,) or t.stride(0) != 1:
-            raise ValueError(name + " must be a contiguous vector of head_dim of the pages' type and device")
+        if (t.dtype != self._dtype or t.get_device() != self._index or t.shape != (self.head_dim,) or t.stride(0) != 1 or
+                t.requires_grad):
+            raise ValueError(name + " must be a contiguous vector of head_dim of the pages' type and device, without "
+                             "gradient")
         return t.data_ptr()
 
     def _q_out(self, q, out):
+        """(heads, rows, row stride, output, its row stride) of q and the given or a new output."""
         heads = q.shape[1] if q.dim() == 3 else 0
         n, qs = self._rows(q, "q", heads)
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            out = torch.empty((n, heads, self.head_dim), dtype=self._dtype, device=q.device)
             return heads, n, qs, out, heads * self.head_dim
-        m, os = self._rows(out, "out", heads)
-        _need(m == n, "out must have q's rows")
+        m, os = self._rows(out, "the output", heads)
+        if m != n:
+            raise ValueError("the output must have q's rows")
         return heads, n, qs, out, os
 
-    def _scale(self, scale):
-        return self.head_dim ** -0.5 if scale is None else scale
-
-    def _workspace(self, desc, prefill, n, window, sinks):
-        """Workspace for one call (None: none needed), from the caching
-        allocator: it is this call's alone on any stream and in any graph."""
-        size = gvc.paged_workspace(desc, prefill, n, window, sinks)
-        return torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
-
     def _call(self, f, *args):
-        if torch.cuda.current_device() != self.device.index:
-            with torch.cuda.device(self.device):
-                return f(*args, torch.cuda.current_stream().cuda_stream)
-        return f(*args, torch.cuda.current_stream().cuda_stream)
+        """f on the current stream of the cache's GPU."""
+        if torch._C._cuda_getDevice() != self._index:
+            with torch.cuda.device(self._index):
+                return f(*args, torch._C._cuda_getCurrentRawStream(self._index))
+        return f(*args, torch._C._cuda_getCurrentRawStream(self._index))
