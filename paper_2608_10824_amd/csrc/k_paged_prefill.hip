@@ -28,6 +28,12 @@ constexpr int kPreUnits = 512;   // calls with fewer units split the slots, into
 constexpr int kPreMinTiles = 4;  // tiles of a part, at least
 constexpr int kPreMaxParts = kPreUnits;
 
+// Kinds of instructions for sched_group_barrier.
+constexpr int kMfma = 0x8, kDsRead = 0x100;
+
+// The lowest n of eight bits, for any n.
+__device__ __forceinline__ uint32_t first8(int n) { return (1u << min(max(n, 0), 8)) - 1; }
+
 // The tile of virtual rows that a workgroup takes.
 struct RowTile {
   int seq, first, begin, rows;   // sequence (-1: none), the tile's first virtual row, the sequence's first row, its virtual rows
@@ -56,11 +62,12 @@ __device__ __forceinline__ RowTile find_tile(const PagedAttnArgs& a, int G, int 
 }
 
 template <class T, int DH>
-__global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const PagedAttnArgs a, float* work, int parts) {
+__global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_prefill(const PagedAttnArgs a, float* work, int parts) {
   constexpr int NK = DH / 16, ND = DH / 32;
   constexpr int CR = DH / 8;               // 16-byte chunks of a key's row
   constexpr int RI = 64 / CR;              // keys of one copy (1 KiB)
-  constexpr int KI = 16 / RI;              // copies of K to a wave (16 keys of the tile), and of V (DH / 4 dimensions)
+  constexpr int KR = kPreKeys / kPreWaves; // keys of a tile that a wave copies
+  constexpr int KI = KR / RI;              // its copies of K, and of V
   constexpr int kTile = kPreKeys * DH * 2; // bytes of K, and of V
   __shared__ __attribute__((aligned(16))) char lds[2][2][kTile];
   const PagedPool& p = a.pool;
@@ -102,7 +109,7 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
   hi_some = uniform(hi_some);
   hi_all = uniform(hi_all);
   lo_some = uniform(a.window ? lo_some - a.window : -1);
-  const int lo_row = a.window ? last - a.window : -1;
+  const int lo_row = a.window ? last - a.window : -1, lo_wg = a.window ? lo - a.window : -1;
   // the workgroup's tiles: the sinks', then the window's; and this part of them
   const int end = (hi >> 6) + 1, win_lo = a.window ? max(lo - a.window + 1, 0) >> 6 : 0;
   const int sink_tiles = a.window ? min((a.n_sinks + 63) >> 6, min(win_lo, end)) : 0;
@@ -126,37 +133,37 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
   // from neighbouring rows hit different banks.
   auto slot_of = [](int n) { return (n & ~12) | ((n & 4) << 1) | ((n & 8) >> 1); };
   const int v_chunk = (lane & 7) ^ (lane >> 3);   // of this lane in every copy of V
-  int k_off[KI];   // elements from the page's row of the wave's first slot
+  const int kw = KR * wv & ~15;   // the 16 slots, always of one page, that the wave's keys are among
+  uint32_t k_off[KI];             // bytes from the first of them
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
-    const int n = i * RI + lane / CR;   // of 16
-    k_off[i] = slot_of(n) * DH + ((lane & (CR - 1)) ^ (n & (CR - 1))) * 8;
+    const int n = (KR * wv & 15) + i * RI + lane / CR;   // of 16
+    k_off[i] = slot_of(n) * DH * 2 + ((lane & (CR - 1)) ^ (n & (CR - 1))) * 16;
   }
-  auto load_ids = [&](int t) {   // the page of chunk v_chunk of tile t
+  auto load_ids = [&](int t) {   // the page of chunk v_chunk of tile t (the last one's past it)
     const int j = tile_slot(min(t, t_end - 1)) + 8 * v_chunk;
     return table[min(j >> p.page_shift, p.max_pages - 1)];
   };
   auto copy = [&](int t, int id) {
-    char* to = lds[t & 1][0];
+    char* to = lds[t & 1][0] + wv * KI * 1024;
     const int j0 = tile_slot(t);
-    const int kid = __builtin_amdgcn_readlane(id, 2 * wv);   // lanes 0 to 7 hold chunks 0 to 7
+    const int kid = __builtin_amdgcn_readlane(id, kw / 8);   // lanes 0 to 7 hold chunks 0 to 7
     const int64_t kb = ((((int64_t)((unsigned)kid < (unsigned)p.n_pages ? kid : 0) * p.Hk + kvh) << p.page_shift) +
-                        ((j0 + 16 * wv) & in_page)) * DH;
+                        ((j0 + kw) & in_page)) * DH;
 #pragma unroll
     for (int i = 0; i < KI; ++i)
-      __builtin_amdgcn_global_load_lds(GPA(p.k + kb + k_off[i]), LPA(to + (wv * KI + i) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(GPA((const char*)(p.k + kb) + k_off[i]), LPA(to + i * 1024), 16, 0, 0);
     const int64_t vb = (((int64_t)((unsigned)id < (unsigned)p.n_pages ? id : 0) * p.Hk + kvh) * DH) << p.page_shift;
     const uint16_t* vp = p.v + vb + ((wv * KI * 8 + (lane >> 3)) << p.page_shift) + ((j0 + 8 * v_chunk) & in_page);
 #pragma unroll
     for (int i = 0; i < KI; ++i)
-      __builtin_amdgcn_global_load_lds(GPA(vp + ((8 * i) << p.page_shift)), LPA(to + kTile + (wv * KI + i) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(GPA(vp + ((8 * i) << p.page_shift)), LPA(to + kTile + i * 1024), 16, 0, 0);
   };
-  // where this lane's operands start
-  int k_at[NK], v_at[4];
-#pragma unroll
-  for (int kk = 0; kk < NK; ++kk) k_at[kk] = r32 * (CR * 16) + (((2 * kk + half) ^ (r32 & (CR - 1))) << 4);
-#pragma unroll
-  for (int m = 0; m < 4; ++m) v_at[m] = kTile + r32 * 128 + (((2 * m + half) ^ (r32 & 7)) << 4);
+  // Where this lane's operands start in a stage: K's chunk 2 kk + half is at
+  // k_at ^ (kk << 5), V's chunk 2 m + half at v_at ^ (m << 5).
+  const int k_at = r32 * (CR * 16) + ((half ^ (r32 & (CR - 1))) << 4);
+  const int v_at = kTile + r32 * 128 + ((half ^ (r32 & 7)) << 4);
+  auto operand = [&](int at) { return *(const pu32x4*)((const char*)lds + at); };
 
   pf32x16 acc[ND];
   float m_run = -INFINITY, l_run = 0.f;   // maximum (powers of two), this lane's share of the sum
@@ -186,33 +193,52 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
     const int j0 = tile_slot(t);
     const unsigned pages = (unsigned)ok & 0xff;   // of the tile's chunks
     ok = next_ok;
+    // Values that no row of the workgroup sees become zeros: what memory holds
+    // there, NaN perhaps, would pass a probability of zero (0 x NaN is NaN).
+    if (pages != 0xff || j0 + 63 > hi || j0 <= lo_wg) {
+#pragma unroll
+      for (int i = 0; i < DH * 8; i += kPreWaves * 64) {
+        pu32x4* v = (pu32x4*)(lds[t & 1][1]) + i + threadIdx.x;
+        const int c = (threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7), j = j0 + 8 * c;
+        uint32_t b = first8(hi + 1 - j) & (~first8(lo_wg + 1 - j) | first8(a.n_sinks - j)) & (0u - ((pages >> c) & 1));
+        pu32x4 keep;
+#pragma unroll
+        for (int w = 0; w < 4; ++w, b >>= 2) keep[w] = (b & 1 ? 0xffffu : 0u) | (b & 2 ? 0xffff0000u : 0u);
+        *v &= keep;
+      }
+      __syncthreads();
+    }
     if (j0 > hi_some || (j0 + 63 <= lo_some && j0 >= a.n_sinks)) continue;   // nothing for this wave
     const bool full = pages == 0xff && j0 + 63 <= hi_all && j0 > lo_all;
-    const char* st = lds[t & 1][0];
+    const int kt = (t & 1) * 2 * kTile + k_at, vt = (t & 1) * 2 * kTile + v_at;
     pf32x16 s[2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[e][i] = 0.f;
+    for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk)
-        s[e] = T::mfma32(*(const pu32x4*)(st + k_at[kk] + e * 32 * CR * 16), qf[kk], s[e]);
+      for (int e = 0; e < 2; ++e) s[e] = T::mfma32(operand((kt ^ (kk << 5)) + e * 32 * CR * 16), qf[kk], s[e]);
+    // four operands ahead of the matrix cores
+    __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * NK; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      if (i < 2 * NK - 4) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
     }
-    uint32_t seen = ~0u, some = ~0u;   // element 16 e + i is slot j0 + 32 e + 16 (i / 8) + 8 half + i % 8
-    if (!full) {
-      seen = some = 0;
+    if (full) {
+      any = true;
+    } else {   // element 16 e + i is slot j0 + 32 e + 16 (i / 8) + 8 half + i % 8
+      uint32_t seen = 0;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int c = 2 * (i >> 3) + half, j = j0 + 8 * c + (i & 7);
-        const bool on = (pages >> c) & 1;
-        const bool in = on & (j <= last) & ((j > lo_row) | (j < a.n_sinks));
-        const bool by = on & (j <= hi_some) & ((j > lo_some) | (j < a.n_sinks));
-        s[i >> 4][i & 15] = in ? s[i >> 4][i & 15] : -INFINITY;
-        seen |= (uint32_t)in << i;
-        some |= (uint32_t)by << i;
+      for (int g = 0; g < 4; ++g) {
+        const int c = 2 * g + half, j = j0 + 8 * c;
+        seen |= (first8(last + 1 - j) & (~first8(lo_row + 1 - j) | first8(a.n_sinks - j)) & (0u - ((pages >> c) & 1)))
+                << (8 * g);
       }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = seen & (1u << i) ? s[i >> 4][i & 15] : -INFINITY;
+      any |= seen != 0;
     }
-    any |= seen != 0;
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
@@ -226,31 +252,30 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[d] *= f;
     }
-    float x[32], sum = 0.f;
+    auto values = [&](int m, pu32x4 (&vf)[ND]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      x[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, shift));
-      sum += x[i];
-    }
-    l_run += sum;
+      for (int d = 0; d < ND; ++d) vf[d] = operand((vt ^ (m << 5)) + d * 32 * 128);
+    };
+    auto weights = [&](int m) {   // probabilities of slots 16 m + 8 half .. + 7, as the operand of the second product
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(s[m >> 1][8 * (m & 1) + i], a.scale_log2e, shift));
+        l_run += x[i];
+      }
+      return pu32x4{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])};
+    };
+    // the next weights are computed while the matrix cores are busy with the last ones
+    pu32x4 vf[2][ND], pf = weights(0);
+    values(0, vf[0]);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      const float* y = x + 8 * m;
-      const pu32x4 pf = {pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]), pack2<T>(y[4], y[5]), pack2<T>(y[6], y[7])};
-      pu32x4 vf[ND];
+      pu32x4 next = pf;
+      if (m < 3) values(m + 1, vf[(m + 1) & 1]);
+      if (m < 3) next = weights(m + 1);
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vf[d] = *(const pu32x4*)(st + v_at[m] + d * 32 * 128);
-      if (!full) {   // values that no row of the wave sees become zeros (0 x NaN is NaN)
-        const uint32_t b = some >> (8 * m);
-        pu32x4 keep;
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          keep[w] = ((b >> (2 * w)) & 1 ? 0xffffu : 0u) | ((b >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) vf[d] &= keep;
-      }
-#pragma unroll
-      for (int d = 0; d < ND; ++d) acc[d] = T::mfma32(vf[d], pf, acc[d]);
+      for (int d = 0; d < ND; ++d) acc[d] = T::mfma32(vf[m & 1][d], pf, acc[d]);
+      pf = next;
     }
   }
   // Where an output is not finite the workgroup does its rows again, slowly: a
@@ -292,7 +317,7 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_paged_prefill(const Paged
         for (int i = 0; i < 16; ++i) s[e][i] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk)
-          s[e] = T::mfma32(*(const pu32x4*)(st + k_at[kk] + e * 32 * CR * 16), qf[kk], s[e]);
+          s[e] = T::mfma32(operand((((t & 1) * 2 * kTile + k_at) ^ (kk << 5)) + e * 32 * CR * 16), qf[kk], s[e]);
       }
       uint32_t seen = 0;
       float top = -INFINITY;
