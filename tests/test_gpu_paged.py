@@ -409,6 +409,226 @@ def test_prefill_of_one_row_is_decode():
     pool.expect(p, q, range(3), [36, 599, 0])
 
 
+# ------------------------------------- prefill: lists long enough for tiles of 128 rows
+def _tiled(pool, rows, heads, window=0, sinks=0):
+    """The calls below are of this kind (what sends them there is in k_paged_decode.hip)."""
+    slots = pool.table.shape[1] * pool.page
+    most = min(window + sinks + 64, slots) if window else slots
+    assert rows * heads * most > 1 << 21 and rows * heads // pool.kv > 16 * pool.table.shape[0]
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv,dh,page,columns", [(28, 4, 128, 16, 0), (40, 1, 64, 32, 0), (32, 16, 64, 128, 0),
+                                                      (27, 1, 128, 64, 0), (6, 2, 128, 16, 90), (5, 1, 64, 128, 12),
+                                                      (4, 4, 64, 16, 180)])
+def test_tiles_of_ragged_rows(t, heads, kv, dh, page, columns):
+    """Whole prompts, one row, no row, chunks behind a cached prefix, rows with
+    gaps, rows in falling order; tables that hold the lengths alone, and such
+    that the slots are split."""
+    pool = Pool(51, t, kv, dh, page, [150, 1, 40, 256, 97, 66], extra_columns=columns)
+    rows = [range(150), [0], [], range(197, 256), sorted(pool.r.permutation(97)[:41]), range(65, -1, -1)]
+    _tiled(pool, sum(len(x) for x in rows), heads)
+    _ragged(pool, heads, rows)
+
+
+@pytest.mark.parametrize("t,dh,page,heads,kv", [("bf16", 64, 16, 128, 2), ("fp16", 128, 64, 120, 1)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (9, 4), (64, 0), (31, 33), (130, 5), (64, 200), (300, 2)])
+def test_tiles_with_window_and_sinks(t, dh, page, heads, kv, window, sinks):
+    pool = Pool(52, t, kv, dh, page, [333, 20, 180])
+    rows = [range(140, 333), range(20), range(0, 180, 3)]
+    _tiled(pool, 273, heads, window, sinks)
+    _ragged(pool, heads, rows, window, sinks)
+
+
+@pytest.mark.parametrize("t,dh,page", [("bf16", 128, 64), ("fp16", 64, 16), ("bf16", 64, 128), ("fp16", 128, 16)])
+def test_tiles_over_many_slots(t, dh, page):
+    """Few tiles over thousands of slots, split and joined: in up to sixteen
+    parts and in more, with and without a window, and rows that see few of them."""
+    pool = Pool(53, t, 1, dh, page, [5100])
+    _tiled(pool, 41, 12)
+    _ragged(pool, 12, [[5099, 0, 300] + list(range(5062, 5100))])
+    _tiled(pool, 90, 16, 1500, 70)
+    _ragged(pool, 16, [range(5010, 5100)], 1500, 70)
+    pool = Pool(54, t, 2, dh, page, [2000, 130, 900])
+    rows = [range(1900, 2000), range(130), [899]]
+    _tiled(pool, 231, 6)
+    _ragged(pool, 6, rows)
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_tiles_where_rows_see_nothing_or_see_each_other(columns):
+    """Empty rows among others and whole tiles of them, an action block whose
+    rows give the block's last slot, rows of no sequence before and behind."""
+    heads = 48 if columns == 0 else 6
+    pool = Pool(55, "bf16", 2, 64, 16, [256, 60], extra_columns=columns)
+    lasts = [5] * 7 + [-1, 3, -1, 49] + list(range(90)) + [99] * 30 + [-1] * 90 + [7, -9, 59] + [8] * 6
+    n = len(lasts)
+    q = pool.rows(n, heads)
+    _tiled(pool, n, heads)
+    held = torch.full((n, heads, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    out = pool.cache.prefill(q, pool.ints(lasts), pool.ints([7, n - 9, n - 6]), out=held)
+    assert (held[:7] == 5).all() and (held[n - 6:] == 5).all()
+    pool.expect(out[7:n - 6], q[7:n - 6], [0] * (n - 16) + [1] * 3, lasts[7:n - 6])
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_tiles_with_pages_that_do_not_exist(columns):
+    heads = 48 if columns == 0 else 6
+    pool = Pool(56, "fp16", 1, 64, 16, [256, 128, 64], extra_columns=columns)
+    c = pool.cache
+    for s, col, to in ((0, 0, -1), (0, 3, c.k_pages.shape[0]), (0, 9, -2 ** 31), (1, 2, 2 ** 31 - 1), (2, 0, -7),
+                       (2, 1, -1), (2, 2, -1), (2, 3, -1)):
+        pool.table[s, col] = to
+    c.page_table.copy_(torch.tensor(pool.table))
+    _tiled(pool, 250, heads)
+    _, out, _, _, _ = _ragged(pool, heads, [range(106, 256), range(40, 128), range(52, 64)])
+    assert not out[238:].any()
+    # a length over what the table holds ends at the table's last slot
+    last = pool.table.shape[1] * 16 - 1
+    q = pool.rows(250, heads)
+    out = c.prefill(q, pool.ints([2 ** 31 - 1, last + 1] * 125), pool.ints([0, 250, 250, 250]))
+    pool.expect(out, q, [0] * 250, [last] * 250)
+
+
+@pytest.mark.parametrize("t,heads,columns,window,sinks", [("bf16", 48, 0, 0, 0), ("fp16", 48, 0, 0, 0), ("bf16", 4, 180, 0, 0),
+                                                          ("fp16", 104, 0, 40, 4), ("bf16", 104, 200, 40, 4)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_tiles_keep_nan_and_infinities_with_the_rows_that_see_them(t, heads, columns, window, sinks, dh):
+    pool = Pool(57, t, 2, dh, 16, [256], extra_columns=columns)
+    c, tb = pool.cache, pool.table
+    c.v_pages[tb[0, 5], 0, 3, 7] = float("nan")    # slot 87
+    c.v_pages[tb[0, 8], 1, 9, 1] = float("inf")    # slot 129
+    c.k_pages[tb[0, 9], 0, 15, 0] = float("nan")   # slot 159
+    _tiled(pool, 256, heads, window, sinks)
+    _, out, _, _, _ = _ragged(pool, heads, [range(256)], window, sinks)
+    o, g = _np(out), heads // 2
+    assert np.isfinite(o[:87]).all() and np.isnan(o[87, :g, 3]).all() and np.isfinite(o[:159, g:, :9]).all()
+    assert np.isinf(o[129, g:, 9]).all() and np.isnan(o[159, :g]).all()
+    if window:
+        assert np.isfinite(o[199:]).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+def test_tiles_of_steep_scores(t):
+    """The running maximum moves up and down over hundreds."""
+    pool = Pool(58, t, 1, 64, 16, [256])
+    for j in range(256):
+        pool.cache.k_pages[pool.table[0, j // 16], 0, j % 16] *= (j % 50) / 10
+    _tiled(pool, 256, 40)
+    _ragged(pool, 40, [range(256)], scale=4.0)
+
+
+def test_tiles_strides_scale_and_out():
+    pool = Pool(59, "bf16", 2, 128, 32, [256])
+    wide = pool.rows(256, 50)
+    q = wide[:, 4:44]
+    held = torch.full((256, 42, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+    _tiled(pool, 256, 40)
+    out = pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3, out=held[:, 1:41])
+    assert (held[:, 0] == 3).all() and (held[:, 41] == 3).all()
+    pool.expect(out, q, [0] * 256, range(256), scale=0.3)
+
+
+def test_captured_tiles_replay_with_other_rows():
+    """A captured call of long lists, split over the slots: rows, bounds and
+    the table change between replays; each is bit for bit the eager result."""
+    pool = Pool(60, "bf16", 2, 64, 16, [1500, 700], spare=30)
+    c = pool.cache
+    n, heads = 400, 8
+    q, last, begin = pool.rows(n, heads), pool.ints([3] * n), pool.ints([0, 200, n])
+    _tiled(pool, n, heads)
+    graphs, outs = [], []
+    c.prefill(q, last, begin)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.prefill(q, last, begin))
+        graphs.append(g)
+    for turn, (cut, a, b) in enumerate([(200, 1499, 699), (350, 1499, 60), (10, 20, 699), (400, 1100, -1)]):
+        q.copy_(pool.rows(n, heads))
+        lasts = [max(a - cut + 1 + i, -1) for i in range(cut)] + [max(b - n + cut + 1 + i, -1) for i in range(n - cut)]
+        last.copy_(pool.ints(lasts))
+        begin.copy_(pool.ints([0, cut, n]))
+        want = c.prefill(q, last, begin)
+        if turn < 2:
+            pick = list(range(0, n, 23)) + [cut - 1, n - 1]
+            pool.expect(want[pick], q[pick], [int(i >= cut) for i in pick], [lasts[i] for i in pick])
+        for g, got in zip(graphs, outs):
+            got.fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(want, got)
+
+
+# ------------------------------------------------------- workspaces of split calls
+def test_a_workspace_may_hold_anything():
+    """Split decodes and prefills through the C ABI, in memory that holds zeros,
+    ones, noise, another call's rest and their own: the same bits."""
+    from paper_2608_10824_amd import gvc
+    pool = Pool(61, "bf16", 2, 128, 16, [4000, 17, 2100, 0])
+    c = pool.cache
+    desc = gvc.PagedDesc(gvc.BF16, 8, 2, 128, 16, c.k_pages.shape[0], 4, c.page_table.shape[1])
+    q, lengths, begin = pool.rows(20, 8), pool.ints([4000, 17, 2100, 0]), pool.ints([0, 1, 2, 20, 20])
+    last = pool.ints([3999, 16] + list(range(2082, 2100)))
+    long_q, long_last, long_begin = pool.rows(300, 8), pool.ints(range(1800, 2100)), pool.ints([0, 0, 0, 300, 300])
+    pages = (c.k_pages.data_ptr(), c.v_pages.data_ptr(), c.page_table.data_ptr())
+    sizes = [gvc.paged_workspace(desc, False, 4), gvc.paged_workspace(desc, True, 20), gvc.paged_workspace(desc, True, 300)]
+    assert min(sizes) > 0
+    work = torch.zeros(max(sizes), dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def run():
+        outs = [torch.empty_like(x) for x in (q[:4], q, long_q)]
+        gvc.paged_decode(desc, 0.09, 0, 0, q.data_ptr(), 1024, lengths.data_ptr(), *pages, outs[0].data_ptr(), 1024,
+                         work.data_ptr(), sizes[0], stream)
+        gvc.paged_prefill(desc, 0.09, 0, 0, q.data_ptr(), 1024, last.data_ptr(), begin.data_ptr(), 20, *pages,
+                          outs[1].data_ptr(), 1024, work.data_ptr(), sizes[1], stream)
+        gvc.paged_prefill(desc, 0.09, 0, 0, long_q.data_ptr(), 1024, long_last.data_ptr(), long_begin.data_ptr(), 300,
+                          *pages, outs[2].data_ptr(), 1024, work.data_ptr(), sizes[2], stream)
+        return outs
+
+    want = run()
+    pool.expect(want[0], q[:4], range(4), [3999, 16, 2099, -1], scale=0.09)
+    pool.expect(want[1], q, [0, 1] + [2] * 18, [3999, 16] + list(range(2082, 2100)), scale=0.09)
+    noise = torch.randint(0, 256, work.shape, dtype=torch.uint8, device=DEV)
+    for fill in (None, 255, 1, noise):
+        if fill is not None:
+            work.copy_(noise) if fill is noise else work.fill_(fill)
+        for x, y in zip(want, run()):
+            assert torch.equal(x, y)
+
+
+def test_a_captured_split_call_after_bounds_that_fall():
+    """What a replay with wrong bounds leaves in the workspace does not reach
+    the next one (few rows, whose parts count each other; bounds that fall can
+    name more parts than the call has)."""
+    from paper_2608_10824_amd.paged import PagedCache
+    pool = Pool(62, "bf16", 1, 64, 16, [2000])
+    n, seqs = 30, 40
+    pool.table = np.repeat(pool.table, seqs, 0)
+    pool.cache = c = PagedCache(pool.cache.k_pages, pool.cache.v_pages, torch.tensor(pool.table, device=DEV))
+    q, last = pool.rows(n, 16), pool.ints([1999] * n)
+    right = [0, 10, 20] + [n] * (seqs - 2)
+    begin = pool.ints(right)
+    assert n * 16 * 2032 < 1 << 21
+    want = c.prefill(q, last, begin)
+    pool.expect(want[::9], q[::9], [0, 0, 1, 2], [1999] * 4)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = c.prefill(q, last, begin)
+    for wrong in ([0, n] * (seqs // 2) + [0], [n, 0] * (seqs // 2) + [n], [0, n, 1, n] * (seqs // 4) + [n]):
+        begin.copy_(pool.ints(wrong))
+        g.replay()
+        torch.cuda.synchronize()
+        begin.copy_(pool.ints(right))
+        got.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want, got)
+
+
 # ----------------------------------------------------------------- together
 def test_a_history_appended_and_attended():
     """Two sequences from an empty cache: a prompt, a second chunk, then single
