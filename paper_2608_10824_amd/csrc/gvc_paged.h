@@ -45,11 +45,17 @@ struct PagedAttnArgs {
   const int* row_begin;   // rows of each sequence, or nullptr: row s is sequence s, and row_last holds lengths
   int n_rows, window, n_sinks;
   float scale_log2e;      // scores in powers of two
+  uint64_t tag;           // of the call (paged_tag)
 };
+
+// A number below 2^52, not zero, that no other call of the process has, and
+// that memory which no call has written holds with a probability of 2^-52.
+uint64_t paged_tag() noexcept;
 
 // How a call is cut into units of work, and the workspace of their partial results.
 struct PagedSplit {
-  bool split;       // a row's slots may be split over units (a second launch joins them)
+  bool split;       // a row's slots may be split over units
+  bool fused;       // decode: the units join their results themselves (else a second launch does)
   int64_t units;    // an upper bound: the grid
   int64_t tiles;    // prefill: row tiles, at most, and the parts that each one's slots are cut into
   int parts;

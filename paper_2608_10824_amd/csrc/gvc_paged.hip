@@ -3,11 +3,37 @@
 #include "gvc_paged.h"
 
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <cmath>
 #include <cstdio>
+#include <random>
 #include <unordered_set>
 
 using namespace gvc;
+
+uint64_t gvc::paged_tag() noexcept {
+  // a permutation of 52 bits (odd multiplications and xor-shifts) of a counter from a random start
+  constexpr uint64_t kMask = ((uint64_t)1 << 52) - 1;
+  static std::atomic<uint64_t> next{[] {
+    uint64_t seed = (uint64_t)std::chrono::steady_clock::now().time_since_epoch().count();
+    try {
+      std::random_device d;
+      seed ^= (uint64_t)d() << 32 ^ d();
+    } catch (...) {   // no entropy source: the clock alone
+    }
+    return seed;
+  }()};
+  for (;;) {
+    uint64_t x = next.fetch_add(1, std::memory_order_relaxed) & kMask;
+    x ^= x >> 27;
+    x = x * 0x9e3779b97f4a7c15u & kMask;
+    x ^= x >> 25;
+    x = x * 0xd1342543de82ef95u & kMask;
+    x ^= x >> 28;
+    if (x) return x;
+  }
+}
 
 namespace {
 
@@ -111,6 +137,7 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.n_rows = n_rows;
   a.window = seen.window;
   a.n_sinks = seen.sinks;
+  a.tag = paged_tag();
   a.scale_log2e = scale * 1.44269504088896340736f;
   bool tiled;
   const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, tiled);
