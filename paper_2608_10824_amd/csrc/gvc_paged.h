@@ -48,8 +48,8 @@ struct PagedAttnArgs {
   uint64_t tag;           // of the call (paged_tag)
 };
 
-// A number below 2^52, not zero, that no other call of the process has, and
-// that memory which no call has written holds with a probability of 2^-52.
+// A number, not zero, that no other call of the process has, and that memory
+// which no call has written holds with a probability of 2^-64.
 uint64_t paged_tag() noexcept;
 
 // How a call is cut into units of work, and the workspace of their partial results.

@@ -13,8 +13,7 @@
 using namespace gvc;
 
 uint64_t gvc::paged_tag() noexcept {
-  // a permutation of 52 bits (odd multiplications and xor-shifts) of a counter from a random start
-  constexpr uint64_t kMask = ((uint64_t)1 << 52) - 1;
+  // a permutation (odd multiplications and xor-shifts) of a counter from a random start
   static std::atomic<uint64_t> next{[] {
     uint64_t seed = (uint64_t)std::chrono::steady_clock::now().time_since_epoch().count();
     try {
@@ -25,12 +24,12 @@ uint64_t gvc::paged_tag() noexcept {
     return seed;
   }()};
   for (;;) {
-    uint64_t x = next.fetch_add(1, std::memory_order_relaxed) & kMask;
-    x ^= x >> 27;
-    x = x * 0x9e3779b97f4a7c15u & kMask;
-    x ^= x >> 25;
-    x = x * 0xd1342543de82ef95u & kMask;
-    x ^= x >> 28;
+    uint64_t x = next.fetch_add(1, std::memory_order_relaxed);
+    x ^= x >> 32;
+    x *= 0x9e3779b97f4a7c15u;
+    x ^= x >> 31;
+    x *= 0xd1342543de82ef95u;
+    x ^= x >> 32;
     if (x) return x;
   }
 }

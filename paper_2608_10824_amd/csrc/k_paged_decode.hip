@@ -36,13 +36,13 @@ constexpr int NW = 4;
 // sequences 143 us against 121), and the least tiles of a chunk: shorter
 // sequences are not split.
 constexpr int kDecTarget = 1024, kDecMinChunk = 16;
-// Chunks that the last workgroup of a row tile joins, at most; more are spread
-// over a second launch's workgroups.  (Against that launch: 32 sequences with a
-// window of 4096 19.9 us for 21.1, 16 of 7B sizes 34.1 for 35.4, and 3 us less of
-// the host's time; 64 long ragged sequences 122.8 for 121.4.)
-constexpr int kFuseChunks = 40;
-constexpr int kTagShift = 12;   // bits of a counter below the tag
-static_assert(kFuseChunks < 1 << kTagShift && 3 * kFuseChunks <= NW / 2 * (64 + 4), "counters, LDS of the fused join");
+// Chunks that the last workgroup of a row tile joins, at most; a second
+// launch spreads more of them over its workgroups, and costs 3 us of the host's time.  (One
+// sequence, 32 heads on 8: 1000 slots 12.4 us against 14.0, 4096, which are 8 chunks,
+// 14.7 against 14.7, 8192 17 against 15; 16 sequences of 500 to 900 slots, 32 heads on
+// 32: 34.3 against 36.2.)
+constexpr int kFuseChunks = 8;
+static_assert(kFuseChunks <= 64, "a lane reads a chunk's flag");
 
 // What rows see whose last slots lie in [least, most], in tiles of 32 slots:
 // tiles [0, sinks) and from `win` on, `count` in all.
@@ -118,44 +118,41 @@ __device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int G, int num
           {uniform(u.rows.begin), uniform(u.rows.rows), uniform(u.rows.last)}};
 }
 
-// A split call's workspace: for each unit and key-value head a counter (of
-// which those of the first chunks are used); for each sequence the number of
-// its first unit and its chunks; then [unit][key-value head][column][DH + 4]
-// floats: maximum, sum, whether a slot was seen, nothing, output.  Columns: G, at
-// most 16, for one row per sequence, else 16.
+// A split call's workspace: for each unit and key-value head a flag; for each
+// sequence the number of its first unit and its chunks; then [unit][key-value
+// head][column][DH + 4] floats: maximum, sum, whether a slot was seen, nothing,
+// output.  Columns: G, at most 16, for one row per sequence, else 16.
 //
-// A counter holds the call's tag and how many chunks are done.  A tag is no
-// other call's (see paged_tag) and the last chunk clears its counter, so what
-// memory holds before does not matter, nor how often a captured call is replayed.
-__host__ __device__ __forceinline__ int64_t counter_bytes(int64_t units) { return (units * 8 + 15) / 16 * 16; }
+// A unit that is done sets its flag to the call's tag, and when the store has
+// come through reads the flags of its row tile's units: the last one finds them
+// all set (two may, and write the same output), and clears them.  A tag is no
+// other call's (see paged_tag), so what memory holds before does not matter, nor how
+// often a captured call is replayed.  (A counter needs read-modify-writes of one
+// address by all units, about 1 us each: 16 chunks took 13 us longer.)
+__host__ __device__ __forceinline__ int64_t flag_bytes(int64_t units) { return (units * 8 + 15) / 16 * 16; }
 __host__ __device__ __forceinline__ int64_t plan_bytes(int n_seqs) { return ((int64_t)n_seqs * 8 + 15) / 16 * 16; }
 __host__ __device__ __forceinline__ int columns(bool rows, int G) { return rows || G > 16 ? 16 : G; }
 
-// Counts a chunk that is done; returns how many are.  Ends: an exchange fails only where another chunk's has succeeded.
-__device__ __forceinline__ int arrive(uint64_t* counter, uint64_t tag, int chunks) {
-  uint64_t old = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), now;
-  do {
-    now = old >> kTagShift == tag ? old + 1 : tag << kTagShift | 1;
-  } while (!__hip_atomic_compare_exchange_strong(counter, &old, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                 __HIP_MEMORY_SCOPE_AGENT));
-  const int n = (int)(now & ((1 << kTagShift) - 1));
-  if (n == chunks) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return n;
+// Partial results and flags pass between XCDs, whose L2 caches do not see each
+// other's lines: they are written and read at agent scope.
+__device__ __forceinline__ void put(uint64_t* to, uint64_t v) {
+  __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-
-// Partial results of the fused join pass between XCDs, whose L2 caches do not
-// see each other's lines: they are written and read at agent scope.
+__device__ __forceinline__ uint64_t get(const uint64_t* from) {
+  return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ void put4(float* to, pf32x4 v) {
   const uint64_t* w = (const uint64_t*)&v;
-  __hip_atomic_store((uint64_t*)to, w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __hip_atomic_store((uint64_t*)to + 1, w[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  put((uint64_t*)to, w[0]);
+  put((uint64_t*)to + 1, w[1]);
 }
 __device__ __forceinline__ pf32x4 get4(const float* from) {
-  const uint64_t x = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const uint64_t y = __hip_atomic_load((const uint64_t*)from + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint64_t x = get((const uint64_t*)from), y = get((const uint64_t*)from + 1);
   return {__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)), __uint_as_float((uint32_t)y),
           __uint_as_float((uint32_t)(y >> 32))};
 }
+// Waits until this wave's stores are where every XCD reads them.
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <class T, int DH, bool ROWS>
 __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs a, char* work, int64_t units, bool fused) {
@@ -168,7 +165,7 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
   const Unit unit = find_unit<ROWS>(a, G, number, lane);
   if (unit.seq < 0) return;   // the grid is an upper bound; uniform over the workgroup
   const int seq = unit.seq, v0 = unit.tile * 16, qs = min(unit.rows.rows - v0, 16);
-  char* plans = work + counter_bytes(units);
+  char* plans = work + flag_bytes(units);
   if (work && !fused && kvh == 0 && unit.index == 0 && unit.tile == 0 && threadIdx.x == 0)
     ((int2*)plans)[seq] = int2{number, unit.count};
   auto row_of = [&](int q) { return ROWS ? unit.rows.begin + (v0 + q) / G : unit.rows.begin; };
@@ -429,46 +426,57 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
       *(pu32x2*)(a.out + row_of(q) * a.out_stride + head_of(q) * DH + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
     } else {
       float* to = parts + ((int64_t)blockIdx.x * columns(ROWS, G) + q) * row_len;
-      put4(to + 4 + d, o);
-      if (d == 0) put4(to, pf32x4{top, ll, saw, 0.f});
+      const pf32x4 stat = {top, ll, saw, 0.f};
+      if (fused) {
+        put4(to + 4 + d, o);
+        if (d == 0) put4(to, stat);
+      } else {
+        *(pf32x4*)(to + 4 + d) = o;
+        if (d == 0) *(pf32x4*)to = stat;
+      }
     }
   }
   const int row_tiles = (unit.rows.rows + 15) >> 4, first = number - unit.index * row_tiles;   // the row tile's first unit
   // (rows' bounds that do not rise can name more units than there are: nobody joins such a tile)
   if (unit.count == 1 || !fused || first + (int64_t)(unit.count - 1) * row_tiles >= units / p.Hk) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's results are where every XCD reads them
+  stores_done();
   __syncthreads();
-  int* last_one = (int*)lds;
-  if (threadIdx.x == 0)
-    *last_one = arrive((uint64_t*)work + (int64_t)first * p.Hk + kvh, a.tag, unit.count) == unit.count;
-  __syncthreads();
-  const bool joins = *last_one != 0;
-  __syncthreads();
-  if (!joins) return;
-  const float* from = parts + ((int64_t)first * p.Hk + kvh) * columns(ROWS, G) * row_len;
-  const int64_t step = (int64_t)row_tiles * p.Hk * columns(ROWS, G) * row_len;   // floats between chunks
-  const int n = unit.count;
-  for (int i = threadIdx.x; i < qs * n; i += NW * 64) {   // maximum, sum and `saw` of column i / n, chunk i % n
-    const pf32x4 x = get4(from + i % n * step + i / n * row_len);
-    lds[3 * i] = x[0];
-    lds[3 * i + 1] = x[1];
-    lds[3 * i + 2] = x[2];
+  int* join = (int*)lds;
+  if (wv == 0) {
+    uint64_t* flags = (uint64_t*)work;
+    if (lane == 0) put(flags + blockIdx.x, a.tag);
+    stores_done();
+    uint64_t* theirs = flags + (first + (int64_t)min(lane, unit.count - 1) * row_tiles) * p.Hk + kvh;   // chunk `lane`'s
+    const bool all = __all(get(theirs) == a.tag);
+    if (all) put(theirs, 0);
+    if (lane == 0) *join = all;
   }
   __syncthreads();
+  if (!*join) return;   // uniform
+  const float* from = parts + ((int64_t)first * p.Hk + kvh) * columns(ROWS, G) * row_len;
+  const int64_t step = (int64_t)row_tiles * p.Hk * columns(ROWS, G) * row_len;   // floats between chunks
   for (int i = threadIdx.x; i < qs * (DH / 4); i += NW * 64) {
     const int q = i / (DH / 4), d = i % (DH / 4) * 4;
-    const float* stat = lds + 3 * q * n;
-    float top = -INFINITY, ll = 0.f, saw = 0.f;
-    for (int c = 0; c < n; ++c) top = fmaxf(top, stat[3 * c]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    pf32x4 o = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) {
-      const float f = __builtin_amdgcn_exp2f(stat[3 * c] - ref);
-      ll += stat[3 * c + 1] * f;
-      saw += stat[3 * c + 2];
-      o += get4(from + c * step + q * row_len + 4 + d) * f;
+    pf32x4 stat[kFuseChunks], x[kFuseChunks];   // all at once: a load takes 1 us
+#pragma unroll
+    for (int c = 0; c < kFuseChunks; ++c) {
+      const float* part = from + min(c, unit.count - 1) * step + q * row_len;
+      stat[c] = get4(part);
+      x[c] = get4(part + 4 + d);
     }
+    float top = -INFINITY, ll = 0.f, saw = 0.f;
+    pf32x4 o = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < kFuseChunks; ++c) top = fmaxf(top, stat[c][0]);   // the last chunk several times is no harm here
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int c = 0; c < kFuseChunks; ++c)
+      if (c < unit.count) {
+        const float f = __builtin_amdgcn_exp2f(stat[c][0] - ref);
+        ll += stat[c][1] * f;
+        saw += stat[c][2];
+        o += x[c] * f;
+      }
     const float inv = 1.f / ll;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
@@ -525,7 +533,7 @@ PagedSplit paged_decode_split(const PagedPool& p, int n_rows, bool rows, int win
   const int64_t by_length = (most + kDecMinChunk - 1) / kDecMinChunk, by_target = kDecTarget / p.Hk + 2;
   s.fused = (by_length < by_target ? by_length : by_target) <= kFuseChunks;
   s.units = tiles * p.Hk + (s.split ? kDecTarget + p.Hk : 0);
-  s.bytes = s.split ? (size_t)(counter_bytes(s.units) + plan_bytes(p.n_seqs) + s.units * columns(rows, G) * (p.dh + 4) * (int64_t)sizeof(float)) : 0;
+  s.bytes = s.split ? (size_t)(flag_bytes(s.units) + plan_bytes(p.n_seqs) + s.units * columns(rows, G) * (p.dh + 4) * (int64_t)sizeof(float)) : 0;
   return s;
 }
 
@@ -535,7 +543,7 @@ static hipError_t decode(const PagedAttnArgs& a, const PagedSplit& sp, void* wor
   char* work = sp.split ? (char*)workspace : nullptr;
   k_paged_decode<T, DH, ROWS><<<(unsigned)sp.units, NW * 64, lds, s>>>(a, work, sp.units, sp.fused);
   if (sp.split && !sp.fused) {
-    const char* plans = work + counter_bytes(sp.units);
+    const char* plans = work + flag_bytes(sp.units);
     const unsigned rows = (unsigned)a.n_rows * a.pool.H;
     const int limit = (int)(sp.units / a.pool.Hk);
     if (rows <= 256) k_paged_join<T, DH, 1024, ROWS><<<rows, 1024, 0, s>>>(a, plans, limit);   // many chunks each
