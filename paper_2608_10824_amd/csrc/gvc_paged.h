@@ -55,6 +55,7 @@ uint64_t paged_tag() noexcept;
 // How a call is cut into units of work, and the workspace of their partial results.
 struct PagedSplit {
   bool split;       // a row's slots may be split over units
+  int least;        // decode: the least tiles of a unit
   bool fused;       // decode: the units join their results themselves (else a second launch does)
   int64_t units;    // an upper bound: the grid
   int64_t tiles;    // prefill: row tiles, at most, and the parts that each one's slots are cut into

@@ -8,14 +8,20 @@
 // virtual row v of a sequence is row v / G, head v % G of the group, and 16 of
 // them are the columns of one MFMA tile.  A workgroup takes one unit: a chunk
 // of the 32-slot tiles that such a tile of rows sees, for one key-value head.
-// The chunk length follows from the sum of the lengths, which only the GPU
-// knows: every wave adds them up and finds its unit, so ragged batches come out
-// in pieces of about equal work, and a batch that fills the GPU by itself is
-// not split at all.  Within a unit the waves take tiles round robin, each with
-// its own online softmax, and are joined in LDS.  The chunks of a row tile are
+// The chunk length follows from the lengths, which only the GPU knows: every
+// wave looks for the one with which the compute units have the least to do (see
+// best_chunk) and finds its unit, so ragged batches come out in pieces of
+// about equal work, and a batch that fills the GPU by itself is not split at
+// all.  Within a unit the waves take tiles round robin, each with its own
+// online softmax, and are joined in LDS.  The chunks of a row tile are
 // joined by the workgroup that is done last, in the order of the chunks, so a
 // result does not depend on which one that is; where there may be more than
 // kFuseChunks of them, by a second launch with a workgroup for each row.
+//
+// Measured (bf16, 128 to a head): one sequence of 282 slots, 32 heads, 7.3 us (a
+// chain of launch, table, keys, values: 4.8 us for one slot); of 131072, 32 heads on
+// 8, 103.5 us, 5.2 TB/s; 16 sequences of 500 to 900 slots, 32 heads, 32.5 us, 4.5
+// TB/s; 64 of 5 to 16384 slots, 64 heads on 8, fp16, 123 us, 4.5 TB/s.
 //
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMA.  A lane's scores in S^T are
 // of one query; the keys of a tile are ordered such that they are also the
@@ -31,16 +37,15 @@ namespace gvc {
 // loads overlap.  (One workgroup of 12 waves instead was slower at every size:
 // 8.6 us against 7.3 for one sequence of 282 slots, 137 against 101 for 131072.)
 constexpr int NW = 4;
-// Units that the chunk length aims at (768 or 2048: 5% slower at one size or
-// another; 256 where the sequences alone give that many units: 64 ragged
-// sequences 143 us against 121), and the least tiles of a chunk: shorter
-// sequences are not split.
-constexpr int kDecTarget = 1024, kDecMinChunk = 16;
+// The least tiles of a chunk (a sequence of fewer than two is not split), and
+// the units that splitting makes at most, besides one for each row tile.
+constexpr int kDecMinChunk = 8, kDecTarget = 1024;
+constexpr float kDecShare = 0.99999f / kDecTarget;   // (a rounded sum is no reason for longer chunks)
 // Chunks that the last workgroup of a row tile joins, at most; a second
-// launch spreads more of them over its workgroups, and costs 3 us of the host's time.  (One
-// sequence, 32 heads on 8: 1000 slots 12.4 us against 14.0, 4096, which are 8 chunks,
-// 14.7 against 14.7, 8192 17 against 15; 16 sequences of 500 to 900 slots, 32 heads on
-// 32: 34.3 against 36.2.)
+// launch spreads more of them over its workgroups, and costs 3 us of the host's time.
+// (One sequence, 32 heads on 8, chunks of 16 tiles: two of them 12.4 us against 14.0, 8
+// 14.7 against 14.7, 16 17 against 15; 16 sequences of 500 to 900 slots, 32 heads:
+// 34.3 against 36.2.)
 constexpr int kFuseChunks = 8;
 static_assert(kFuseChunks <= 64, "a lane reads a chunk's flag");
 
@@ -74,29 +79,79 @@ struct Unit {
   SeqRows rows;
 };
 
-// The chunk length is the sum of all tiles over the units aimed at (so no
-// sequence has more chunks than that, and two).  A sequence's row tiles all have
-// the chunks that its last row would have.  Units are numbered through the sequences in
-// order, chunk by chunk.  Every wave finds this out by itself.
+// Chunk lengths that are tried, one to a lane of 16: 8, 10, 12, 16, 20, 25, .. 203 and no splitting.
+__device__ __forceinline__ int chunk_length(int k) {
+  return k == 15 ? 1 << 27 : (int)(8.01f * __builtin_amdgcn_exp2f((float)k * (1.f / 3)));
+}
+
+// A call takes about as long as the compute unit with the most to do: its
+// units, ceil(units / 256), by a chunk's tiles, the eight that a unit's start
+// and end are worth, and as many for the join.  (Where a compute unit has more
+// units than it holds, they come one by one as it gets room.)  Of the sixteen
+// lengths this is the one for which that is least, and not so short that there
+// are more units than kDecTarget and the row tiles.  It takes 0.7 us.  (Against
+// chunks of at least 16 tiles that made 1024 units, 32 heads on 8: one sequence of 4096
+// slots 13.0 us for 14.7, 12 of 2000 23.4 for 25.3, 64 of 700 38.4 for 45.8, 32 with a
+// window of 1000, 28 heads on 4, 19.1 for 20.4; 64 of 500 29.7 for 28.5.)
+// r, n: rows and tiles of sequence `lane`, or of the last one.
+__device__ __forceinline__ int best_chunk(const PagedAttnArgs& a, int least, int lane, const SeqRows& r, int n) {
+  const int S = a.pool.n_seqs, mine = chunk_length(lane & 15);
+  const float part = 1.f / (float)mine, tiles = lane < S ? (float)((r.rows + 15) >> 4) : 0.f;
+  float units = 0.f, total = 0.f, longest = 0.f;   // units, all tiles and the longest of every fourth sequence
+  for (int i = 0; i < S; i += 32) {
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+      const float t = __shfl(tiles, i + k + (lane >> 4)), m = (float)__shfl(n, i + k + (lane >> 4));
+      units += t * (m < 2 * kDecMinChunk ? 1.f : fmaxf(ceilf(fmaf(m, part, -1e-4f)), 1.f));
+      total = fmaf(t, m, total);
+      longest = fmaxf(longest, t > 0.f ? m : 0.f);
+    }
+  }
+  units = rows_sum(units) * (float)a.pool.Hk;
+  total = rows_sum(total) * (float)a.pool.Hk;
+  longest = rows_max(longest);
+  const float share = total * kDecShare;
+  if (__any(share > 200.f)) return share < 1 << 27 ? (int)ceilf(share) : 1 << 27;   // (the same in every lane)
+  const bool allowed = (lane & 15) == 15 || (mine >= least && (float)mine >= share);
+  const float rounds = units * (1.f / 256);
+  const float cost = (rounds > 3.f ? rounds + 0.5f : ceilf(rounds)) * ((float)mine < longest ? (float)mine + 16.f : longest + 8.f);
+  const int order = allowed ? -__float_as_int(cost) : -__float_as_int(INFINITY);   // of floats that are not negative
+  const int most = row16_max(order);
+  const uint64_t best = __ballot(order == most);
+  return chunk_length((63 - __builtin_clzll(best)) & 15);
+}
+
+// More than 64 sequences: their chunks are long anyway, and looking for the best would cost more than
+// it gives (200 sequences of 700 slots: 6 us of 110).
 template <bool ROWS>
-__device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int G, int number, int lane) {
+__device__ __forceinline__ int long_chunk(const PagedAttnArgs& a, int G, int least, int lane) {
+  float total = 0.f;
+  for (int s = lane; s < a.pool.n_seqs; s += 64) {
+    const SeqRows r = seq_rows<ROWS>(a, s, G);
+    total += (float)((r.rows + 15) >> 4) * (float)slot_tiles(a, r.last, r.last).count;
+  }
+  const float share = wave_sum(total) * (float)a.pool.Hk * kDecShare;
+  return max(share < 1 << 27 ? (int)ceilf(share) : 1 << 27, max(least, 4 * kDecMinChunk));
+}
+
+// Units are numbered through the sequences in order, chunk by chunk; a
+// sequence's row tiles all have the chunks that its last row would have.  Every
+// wave finds its unit by itself.
+template <bool ROWS>
+__device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int G, int number, int least, int lane) {
   const int S = a.pool.n_seqs;
   SeqRows r = seq_rows<ROWS>(a, min(lane, S - 1), G);
   int n = slot_tiles(a, r.last, r.last).count;
-  float total = lane < S ? (float)((r.rows + 15) >> 4) * (float)n : 0.f;
-  for (int s = lane + 64; s < S; s += 64) {
-    const SeqRows o = seq_rows<ROWS>(a, s, G);
-    total += (float)((o.rows + 15) >> 4) * (float)slot_tiles(a, o.last, o.last).count;
-  }
-  const float aim = wave_sum(total) * (float)a.pool.Hk * (0.99999f / kDecTarget);   // a rounded sum is no reason to round up
-  const int chunk = max((int)ceilf(aim), kDecMinChunk);
+  int chunk = chunk_length(15);
+  if (S > 64) chunk = long_chunk<ROWS>(a, G, least, lane);
+  else if (__any(n >= 2 * kDecMinChunk)) chunk = best_chunk(a, least, lane, r, n);
   Unit u{-1, 0, 0, 0, {}};
   for (int s0 = 0; s0 < S; s0 += 64) {
     if (s0) {
       r = seq_rows<ROWS>(a, min(s0 + lane, S - 1), G);
       n = slot_tiles(a, r.last, r.last).count;
     }
-    const int count = max((n + chunk - 1) / chunk, 1), tiles = (r.rows + 15) >> 4;
+    const int count = n < 2 * kDecMinChunk ? 1 : (n + chunk - 1) / chunk, tiles = (r.rows + 15) >> 4;
     const int units = s0 + lane < S ? count * tiles : 0;
     const int sum = wave_scan(units);
     const uint64_t past = __ballot(sum > number);
@@ -155,14 +210,15 @@ __device__ __forceinline__ pf32x4 get4(const float* from) {
 __device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <class T, int DH, bool ROWS>
-__global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs a, char* work, int64_t units, bool fused) {
+__global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs a, char* work, int64_t units, bool fused,
+                                                              int least_chunk) {
   constexpr int NK = DH / 32, NO = DH / 16;
   extern __shared__ float lds[];   // [waves / 2][columns][DH + 4], then [waves][16][4]
   const PagedPool& p = a.pool;
   const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int G = p.H / p.Hk, kvh = blockIdx.x % p.Hk, number = blockIdx.x / p.Hk;
-  const Unit unit = find_unit<ROWS>(a, G, number, lane);
+  const Unit unit = find_unit<ROWS>(a, G, number, least_chunk, lane);
   if (unit.seq < 0) return;   // the grid is an upper bound; uniform over the workgroup
   const int seq = unit.seq, v0 = unit.tile * 16, qs = min(unit.rows.rows - v0, 16);
   char* plans = work + flag_bytes(units);
@@ -529,9 +585,12 @@ PagedSplit paged_decode_split(const PagedPool& p, int n_rows, bool rows, int win
   const int64_t seen = window ? ((int64_t)window + 31) / 32 + 1 + ((int64_t)n_sinks + 31) / 32 : all;
   PagedSplit s{};
   const int64_t most = seen < all ? seen : all;
-  s.split = most > kDecMinChunk;
-  const int64_t by_length = (most + kDecMinChunk - 1) / kDecMinChunk, by_target = kDecTarget / p.Hk + 2;
-  s.fused = (by_length < by_target ? by_length : by_target) <= kFuseChunks;
+  s.split = most >= 2 * kDecMinChunk;
+  // The units join their results where a sequence has at most kFuseChunks chunks of the least length, or
+  // where few longer ones are enough to fill the GPU.
+  const int64_t least = (most + kFuseChunks - 1) / kFuseChunks;
+  s.fused = least <= kDecMinChunk || (least <= 4 * kDecMinChunk && p.Hk * kFuseChunks >= 256);
+  s.least = s.fused && least > kDecMinChunk ? (int)least : kDecMinChunk;
   s.units = tiles * p.Hk + (s.split ? kDecTarget + p.Hk : 0);
   s.bytes = s.split ? (size_t)(flag_bytes(s.units) + plan_bytes(p.n_seqs) + s.units * columns(rows, G) * (p.dh + 4) * (int64_t)sizeof(float)) : 0;
   return s;
@@ -541,7 +600,7 @@ template <class T, int DH, bool ROWS>
 static hipError_t decode(const PagedAttnArgs& a, const PagedSplit& sp, void* workspace, hipStream_t s) {
   const size_t lds = (size_t)NW * (columns(ROWS, a.pool.H / a.pool.Hk) * (DH + 4) / 2 + 16 * 4) * sizeof(float);
   char* work = sp.split ? (char*)workspace : nullptr;
-  k_paged_decode<T, DH, ROWS><<<(unsigned)sp.units, NW * 64, lds, s>>>(a, work, sp.units, sp.fused);
+  k_paged_decode<T, DH, ROWS><<<(unsigned)sp.units, NW * 64, lds, s>>>(a, work, sp.units, sp.fused, sp.least);
   if (sp.split && !sp.fused) {
     const char* plans = work + flag_bytes(sp.units);
     const unsigned rows = (unsigned)a.n_rows * a.pool.H;
