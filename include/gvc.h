@@ -372,7 +372,8 @@ int32_t gvc_destroy(gvc_ctx* ctx);
  * multiples of 8.  Scores, softmax statistics and norms are fp32.  Calls are
  * asynchronous on `stream` (NULL = the null stream) of the current GPU, may
  * be captured into a graph, and run on several streams at once if their
- * workspaces, outputs and written slots are apart.  No call allocates device memory. */
+ * workspaces, outputs and written slots are apart.  out may be q itself (address
+ * and stride), else must not overlap the inputs.  No call allocates device memory. */
 enum gvc_dtype { GVC_BF16 = 0, GVC_FP16 = 1 };
 
 typedef struct gvc_paged_desc {
@@ -410,9 +411,9 @@ typedef struct gvc_paged_rope {
  * slot or page does not exist (a padding row: sequence -1) writes no slot; its
  * q_out is written all the same.  Two rows of one call must not name the same
  * slot (gvc_paged_check finds that), else either may be left there, element by
- * element.  q and q_out may both be NULL (keys and values only).  q_out must
- * not overlap the inputs.  n_rows * (n_heads + 2 n_kv_heads) < 2^28.  Errors:
- * GVC_EINVAL, GVC_EDEVICE. */
+ * element.  q and q_out may both be NULL (keys and values only).  q_out may be
+ * q itself (address and stride), else must not overlap the inputs.  n_rows *
+ * (n_heads + 2 n_kv_heads) < 2^28.  Errors: GVC_EINVAL, GVC_EDEVICE. */
 int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
                          const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,

@@ -22,7 +22,7 @@ struct PagedPool {
 };
 
 constexpr int kPagedMaxPairs = 64;   // head_dim / 2
-constexpr int kPagedMaxSeqs = 4096;  // their first tiles are kept in LDS
+constexpr int kPagedMaxSeqs = 4096;  // every wave goes through their rows to find its work
 
 struct PagedAppendArgs {
   PagedPool pool;
@@ -88,7 +88,11 @@ typedef uint16_t pu16x8 __attribute__((ext_vector_type(8)));
 // and sum are rescaled: a probability is at most 2^kPagedLazy, far from overflow.
 constexpr float kPagedLazy = 8.f;
 
-// The two 16-bit types.  Conversions to 16 bits round to nearest even.
+// The two 16-bit types.  Conversions to 16 bits round to nearest even.  What is
+// rounded to them, once each: a rotated query or key (the pages hold 16 bits), a
+// probability before the second product (whose operands are of one type: half a
+// step, 2^-9 of it in bf16, averages out over the slots; the sum takes it
+// unrounded) and an output.
 struct Bf16 {
   typedef __bf16 elem;
   typedef pbf16x8 x8;

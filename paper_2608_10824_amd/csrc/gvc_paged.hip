@@ -117,7 +117,8 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
                const void* v_pages, const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
                size_t workspace_bytes, void* stream) noexcept {
   const gvc_paged_desc& d = *desc;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail("scale must be positive and finite");
+  const float scale_log2e = scale * 1.44269504088896340736f;
+  if (!(scale > 0.f) || !std::isfinite(scale_log2e)) return fail("scale must be positive and finite (in powers of two too)");
   if (const char* w = bad_reach(window, n_sinks)) return fail(w);
   if (n_rows == 0) return GVC_OK;
   if (!row_last || !k_pages || !v_pages || !page_table) return fail("null argument");
@@ -137,7 +138,7 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.window = seen.window;
   a.n_sinks = seen.sinks;
   a.tag = paged_tag();
-  a.scale_log2e = scale * 1.44269504088896340736f;
+  a.scale_log2e = scale_log2e;
   bool tiled;
   const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, tiled);
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))

@@ -54,6 +54,8 @@ class PagedCache:
             raise ValueError("v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
         if page_table.dtype != torch.int32 or page_table.dim() != 2:
             raise ValueError("page_table must be int32 [n_seqs][max_pages]")
+        if k_pages.requires_grad or v_pages.requires_grad:
+            raise ValueError("pages must not require a gradient")
         if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous()):
             raise ValueError("pages and page table must be contiguous")
         index = k_pages.get_device()
@@ -83,7 +85,7 @@ class PagedCache:
         [rows][n_heads][head_dim] normalised and rotated (None for q None).
         rope_pairs: rotated pairs of each axis, at most three (default: the
         whole head on one axis; () rotates nothing); positions: int32
-        [axes][rows], default the slots."""
+        [axes][rows], default the slots.  q_out may be q itself."""
         kv = self.n_kv_heads
         n, ks = self._rows(k, "k", kv)
         m, vs = self._rows(v, "v", kv)
@@ -119,7 +121,7 @@ class PagedCache:
     def decode(self, q, lengths, *, scale=None, window=0, sinks=0, out=None):
         """Attention of one token per sequence: q [n_seqs][n_heads][head_dim],
         row s over the first lengths[s] slots (int32; 0: an idle slot of the
-        batch, zeros).  scale: default head_dim^-1/2."""
+        batch, zeros).  scale: default head_dim^-1/2.  out may be q itself."""
         heads, n, qs, out, os = self._q_out(q, out)
         if n != self.n_seqs:
             raise ValueError("q must have one row per sequence")
@@ -135,7 +137,8 @@ class PagedCache:
         """Attention of rows q [rows][n_heads][head_dim]: rows row_begin[s] to
         row_begin[s + 1] - 1 (int32 [n_seqs + 1]) are sequence s's, and row r
         sees slots up to row_last[r] (int32; -1: none).  Rows of no sequence
-        are left as they are in `out` (undefined in a new one)."""
+        are left as they are in `out` (undefined in a new one), which may be q
+        itself."""
         heads, n, qs, out, os = self._q_out(q, out)
         self._ints(row_last, "row_last", n)
         self._ints(row_begin, "row_begin", self.n_seqs + 1)
@@ -172,8 +175,11 @@ class PagedCache:
     def _workspace(self, desc, heads, prefill, n, window, sinks):
         """Workspace for one call (None: none needed), from the caching
         allocator: it is this call's alone on any stream and in any graph."""
-        size = _kept(_sizes, (self._shape, heads, prefill, n, window, sinks),
-                     lambda: gvc.paged_workspace(desc, prefill, n, window, sinks))
+        def make():
+            if not (-2 ** 31 <= window < 2 ** 31 and -2 ** 31 <= sinks < 2 ** 31):   # the C call would see other numbers
+                raise ValueError("window and sinks must fit 32 bits")
+            return gvc.paged_workspace(desc, prefill, n, window, sinks)
+        size = _kept(_sizes, (self._shape, heads, prefill, n, window, sinks), make)
         return torch.empty(size, dtype=torch.uint8, device=self.k_pages.device) if size else None
 
     def _rows(self, t, name, heads):

@@ -409,6 +409,39 @@ def test_prefill_of_one_row_is_decode():
     pool.expect(p, q, range(3), [36, 599, 0])
 
 
+@pytest.mark.parametrize("seqs,heads,kv", [(64, 4, 2), (65, 6, 2), (130, 2, 1)])
+def test_decode_many_sequences(seqs, heads, kv):
+    """Ragged batches of 64 sequences and more, idle ones among them; rows of the same as a prefill."""
+    r = np.random.default_rng(41)
+    lengths = [int(n) for n in np.where(r.random(seqs) < 0.2, 0, np.exp(r.uniform(0, 7, seqs)))]
+    pool = Pool(41, "bf16", kv, 64, 16, lengths)
+    q = pool.rows(seqs, heads)
+    out = pool.cache.decode(q, pool.ints(lengths))
+    pool.expect(out, q, range(seqs), [n - 1 for n in lengths])
+    out = pool.cache.decode(q, pool.ints(lengths), window=333, sinks=20)
+    pool.expect(out, q, range(seqs), [n - 1 for n in lengths], 333, 20)
+    if seqs * kv <= 130:
+        rows = [[n - 1, n // 2][:int(r.integers(0, 3))] if n else [] for n in lengths]
+        _ragged(pool, heads, rows)
+
+
+@pytest.mark.parametrize("seqs,kv,length", [(64, 8, 30000), (70, 2, 30000), (3, 8, 70000)])
+def test_decode_long_sequences_on_the_same_pages(seqs, kv, length):
+    """Lengths at which chunks are hundreds of tiles; all tables name the pages of one small pool."""
+    from paper_2608_10824_amd.paged import PagedCache
+    page, n_pages = 128, 40
+    pool = Pool(42, "fp16", kv, 64, page, [page * n_pages], spare=0, extra_columns=0)
+    columns = -(-length // page)
+    pool.table = pool.r.integers(0, n_pages, (seqs, columns)).astype(np.int32)
+    pool.cache = c = PagedCache(pool.cache.k_pages, pool.cache.v_pages, torch.tensor(pool.table, device=DEV))
+    lengths = [int(length * f) for f in np.linspace(0.6, 1, seqs)]
+    lengths[1] = 5
+    q = pool.rows(seqs, kv)
+    out = c.decode(q, pool.ints(lengths))
+    pick = [0, 1, seqs // 2, seqs - 1]
+    pool.expect(out[pick], q[pick], pick, [lengths[i] - 1 for i in pick])
+
+
 # ------------------------------------- prefill: lists long enough for tiles of 128 rows
 def _tiled(pool, rows, heads, window=0, sinks=0):
     """The calls below are of this kind (what sends them there is in k_paged_decode.hip)."""
@@ -750,6 +783,44 @@ def test_pool_over_four_gib():
     begin = torch.tensor([0, 2, 3], dtype=torch.int32, device=DEV)
     qp = q[:3].contiguous()
     assert torch.equal(c.prefill(qp, last, begin), small.prefill(qp, last, begin))
+
+
+def test_outputs_in_place_of_their_inputs():
+    """q_out or out may be q itself: rotation, unsplit and split decodes and
+    lists of rows of both kinds give the same bits."""
+    pool = Pool(37, "bf16", 2, 64, 16, [1500, 40, 0])
+    c, n = pool.cache, 300
+    x = pool.rows(n, 12)
+    seq, slot = pool.ints([0] * n), pool.ints(range(1200, 1500))
+    want = c.append(x[:, :8], x[:, 8:10], x[:, 10:], seq, slot)
+    got = x.clone()
+    c.append(got[:, :8], got[:, 8:10], got[:, 10:], seq, slot, q_out=got[:, :8])
+    assert torch.equal(want, got[:, :8]) and torch.equal(x[:, 8:], got[:, 8:])
+    for f in (lambda q, o: c.decode(q, pool.ints([1500, 40, 0]), out=o), lambda q, o: c.decode(q, pool.ints([300, 40, 0]), out=o),
+              lambda q, o: c.prefill(q, pool.ints([1499, 39, 7]), pool.ints([0, 1, 3, 3]), out=o)):
+        q = pool.rows(3, 8)
+        want = f(q, None)
+        assert torch.equal(f(q, q), want)
+    q = pool.rows(n, 8)
+    _tiled(pool, n, 8)
+    want = c.prefill(q, slot, pool.ints([0, n, n, n]))
+    assert torch.equal(c.prefill(q, slot, pool.ints([0, n, n, n]), out=q), want)
+    pool = Pool(38, "fp16", 1, 128, 32, [256], extra_columns=0)
+    q, slot = pool.rows(256, 40), pool.ints(range(256))
+    _tiled(pool, 256, 40)
+    want = pool.cache.prefill(q, slot, pool.ints([0, 256]))
+    assert torch.equal(pool.cache.prefill(q, slot, pool.ints([0, 256]), out=q), want)
+
+
+def test_more_wrapper_refusals():
+    from paper_2608_10824_amd.paged import PagedCache
+    pool = Pool(39, "bf16", 2, 64, 16, [20, 20])
+    c, q, two = pool.cache, pool.rows(2, 4), pool.ints([3, 4])
+    for f in (lambda: c.decode(q, two, window=2 ** 32 + 5), lambda: c.decode(q, two, sinks=2 ** 31),
+              lambda: c.prefill(q, two, pool.ints([0, 1, 2]), window=2 ** 31),
+              lambda: PagedCache(c.k_pages.clone().requires_grad_(), c.v_pages, c.page_table)):
+        with pytest.raises(ValueError):
+            f()
 
 
 def test_wrapper_refusals():

@@ -84,7 +84,7 @@ def test_bad_append_refused(kw):
 
 
 @pytest.mark.parametrize("call", [_decode, _prefill])
-@pytest.mark.parametrize("kw", [dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+@pytest.mark.parametrize("kw", [dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
                                 dict(window=-1), dict(sinks=-1), dict(q=None), dict(kp=None), dict(vp=None),
                                 dict(table=None), dict(o=None), dict(q=P + 8), dict(o=P + 2), dict(vp=P + 2),
                                 dict(qs=508), dict(os=448)])
