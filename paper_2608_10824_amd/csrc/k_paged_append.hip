@@ -18,6 +18,11 @@
 //    rows fill eight slots in a row, a lane writes 16 bytes of one dimension;
 //    rows that stand alone are written in 2-byte pieces, neighbouring lanes
 //    taking neighbouring rows, so that pieces of one page meet in a cache line.
+//
+// Measured (bf16, 128 to a head): 19600 rows of whole prompts, 32 heads on 8, norm
+// and three axes 107 us, 4.5 TB/s read and written, 88% of a copy; 2368 rows of 16
+// sequences, about every second slot, 32 heads 36 us, 3.2 TB/s (parts of
+// V's 32-byte sectors: 75 MB written for 58); one row 3.7 us.
 #include "gvc_kernels.h"
 #include "gvc_paged.h"
 
