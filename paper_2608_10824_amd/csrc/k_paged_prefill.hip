@@ -16,14 +16,17 @@
 // values of few heads.  Few rows over many slots are split over the slots as
 // well; a second launch joins the parts.
 //
-// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 541 us, 1015 TFLOP/s of
-// the products that rows see, 83% of a large matrix product's rate (matrix cores busy 48%,
-// vector units 46% of the time: the softmax costs as much as the products, and
-// the two take turns); heads of 64 318 us, 865 TFLOP/s; 4 prompts of 1000 rows 60 us.
+// The copies go by buffer loads: beside loads of the other kind into LDS the compiler
+// waits for all LDS reads where it needs one (5% slower), and a page's address
+// stays in scalar registers.
+//
+// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 533 us, 1032 TFLOP/s of
+// the products that rows see, 85% of a large matrix product's rate (matrix cores busy 51%,
+// vector units 45% of the time: the softmax costs as much as the products, and
+// the two take turns); heads of 64 312 us, 881 TFLOP/s; 4 prompts of 1000 rows 58 us.
 #include "gvc_paged_rows.h"
 #include "gvc_sync.h"
 
-#define GPA(p) ((const void __attribute__((address_space(1)))*)(p))
 #define LPA(p) ((void __attribute__((address_space(3)))*)(p))
 
 namespace gvc {
@@ -132,42 +135,42 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
 #pragma unroll
   for (int kk = 0; kk < NK; ++kk) qf[kk] = *(const pu32x4*)(a.q + row * a.q_stride + h * DH + kk * 16 + half * 8);
 
-  // Copies.  K: LDS row n of a tile holds slot slot_of(n), the order of the
-  // operand's rows; chunk c of it is at c ^ n (mod CR).  V: dimension d's eight
-  // chunks of eight slots, chunk c at c ^ d (mod 8).  So lanes that read an operand
-  // from neighbouring rows hit different banks.
+  // Copies, of the 16 slots (always of one page) that are the wave's in every
+  // tile.  K: LDS row n of a tile holds slot slot_of(n), the order of the operand's
+  // rows; chunk c (16 bytes) of it is at c ^ turn(n).  V: a copy is one operand, 32
+  // dimensions of two chunks of eight slots; chunk c of dimension d is at c ^ (d / 8 & 1).  So
+  // sixteen lanes that read an operand together hit different banks.
   auto slot_of = [](int n) { return (n & ~12) | ((n & 4) << 1) | ((n & 8) >> 1); };
-  const int v_chunk = (lane & 7) ^ (lane >> 3);   // of this lane in every copy of V
-  const int kw = KR * wv & ~15;   // the 16 slots, always of one page, that the wave's keys are among
-  uint32_t k_off[KI];             // bytes from the first of them
+  auto turn = [](int n) { return DH == 64 ? n >> 1 & 7 : n & 15; };
+  uint32_t k_off[KI];             // bytes from the first slot's
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
-    const int n = (KR * wv & 15) + i * RI + lane / CR;   // of 16
-    k_off[i] = slot_of(n) * DH * 2 + ((lane & (CR - 1)) ^ (n & (CR - 1))) * 16;
+    const int n = i * RI + lane / CR;
+    k_off[i] = slot_of(n) * DH * 2 + ((lane & (CR - 1)) ^ turn(n)) * 16;
   }
-  auto load_ids = [&](int t) {   // the page of chunk v_chunk of tile t (the last one's past it)
-    const int j = tile_slot(min(t, t_end - 1)) + 8 * v_chunk;
+  const uint32_t v_off = ((lane >> 1) << (p.page_shift + 1)) + ((lane & 1) ^ (lane >> 4 & 1)) * 16;
+  auto load_ids = [&](int t) {   // the page of chunk lane % 8 of tile t (the last one's past it)
+    const int j = tile_slot(min(t, t_end - 1)) + 8 * (lane & 7);
     return table[min(j >> p.page_shift, p.max_pages - 1)];
   };
+  const int head_bytes = (DH * 2) << p.page_shift;   // of a page
   auto copy = [&](int t, int id) {
     char* to = lds[t & 1][0] + wv * KI * 1024;
-    const int j0 = tile_slot(t);
-    const int kid = __builtin_amdgcn_readlane(id, kw / 8);   // lanes 0 to 7 hold chunks 0 to 7
-    const int64_t kb = ((((int64_t)((unsigned)kid < (unsigned)p.n_pages ? kid : 0) * p.Hk + kvh) << p.page_shift) +
-                        ((j0 + kw) & in_page)) * DH;
+    const int page = __builtin_amdgcn_readlane(id, 2 * wv), off = (tile_slot(t) + 16 * wv) & in_page;
+    const int64_t at = ((int64_t)((unsigned)page < (unsigned)p.n_pages ? page : 0) * p.Hk + kvh) * head_bytes;
+    const auto k = __builtin_amdgcn_make_buffer_rsrc((char*)p.k + at, (short)0, head_bytes, 0x00020000);
+    const auto v = __builtin_amdgcn_make_buffer_rsrc((char*)p.v + at, (short)0, head_bytes, 0x00020000);
 #pragma unroll
     for (int i = 0; i < KI; ++i)
-      __builtin_amdgcn_global_load_lds(GPA((const char*)(p.k + kb) + k_off[i]), LPA(to + i * 1024), 16, 0, 0);
-    const int64_t vb = (((int64_t)((unsigned)id < (unsigned)p.n_pages ? id : 0) * p.Hk + kvh) * DH) << p.page_shift;
-    const uint16_t* vp = p.v + vb + ((wv * KI * 8 + (lane >> 3)) << p.page_shift) + ((j0 + 8 * v_chunk) & in_page);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(k, LPA(to + i * 1024), 16, (int)k_off[i], off * DH * 2, 0, 0);
 #pragma unroll
     for (int i = 0; i < KI; ++i)
-      __builtin_amdgcn_global_load_lds(GPA(vp + ((8 * i) << p.page_shift)), LPA(to + kTile + i * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(v, LPA(to + kTile + i * 1024), 16, (int)v_off, (i << (p.page_shift + 6)) + off * 2, 0, 0);
   };
   // Where this lane's operands start in a stage: K's chunk 2 kk + half is at
-  // k_at ^ (kk << 5), V's chunk 2 m + half at v_at ^ (m << 5).
-  const int k_at = r32 * (CR * 16) + ((half ^ (r32 & (CR - 1))) << 4);
-  const int v_at = kTile + r32 * 128 + ((half ^ (r32 & 7)) << 4);
+  // k_at ^ (kk << 5), V's chunk half of slots 16 m.. and dimensions 32 d.. 1024 (ND m + d) behind v_at.
+  const int k_at = r32 * (CR * 16) + ((half ^ turn(r32)) << 4);
+  const int v_at = kTile + r32 * 32 + ((half ^ (r32 >> 3 & 1)) << 4);
   auto operand = [&](int at) { return *(const pu32x4*)((const char*)lds + at); };
 
   pf32x16 acc[ND];
@@ -204,14 +207,15 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
 #pragma unroll
       for (int i = 0; i < DH * 8; i += kPreWaves * 64) {
         pu32x4* v = (pu32x4*)(lds[t & 1][1]) + i + threadIdx.x;
-        const int c = (threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7), j = j0 + 8 * c;
+        const int c = 2 * ((i + threadIdx.x) / (64 * ND)) + ((threadIdx.x & 1) ^ (threadIdx.x >> 4 & 1)), j = j0 + 8 * c;
         uint32_t b = first8(hi + 1 - j) & (~first8(lo_wg + 1 - j) | first8(a.n_sinks - j)) & (0u - ((pages >> c) & 1));
         pu32x4 keep;
 #pragma unroll
         for (int w = 0; w < 4; ++w, b >>= 2) keep[w] = (b & 1 ? 0xffffu : 0u) | (b & 2 ? 0xffff0000u : 0u);
         *v &= keep;
       }
-      __syncthreads();
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // LDS only: the next tile's copies go on
+      lds_barrier();
     }
     if (j0 > hi_some || (j0 + 63 <= lo_some && j0 >= a.n_sinks)) continue;   // nothing for this wave
     const bool full = pages == 0xff && j0 + 63 <= hi_all && j0 > lo_all;
@@ -259,7 +263,7 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
     }
     auto values = [&](int m, pu32x4 (&vf)[ND]) {
 #pragma unroll
-      for (int d = 0; d < ND; ++d) vf[d] = operand((vt ^ (m << 5)) + d * 32 * 128);
+      for (int d = 0; d < ND; ++d) vf[d] = operand(vt + (m * ND + d) * 1024);
     };
     auto weights = [&](int m) {   // probabilities of slots 16 m + 8 half .. + 7, as the operand of the second product
       float x[8];
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
                 const int dim = 32 * d + 8 * (k >> 2) + 4 * half + (k & 3);
-                const char* vp = st + kTile + dim * 128 + (((2 * m + o) ^ (dim & 7)) << 4) + 2 * j;
+                const char* vp = st + kTile + (m * ND + d) * 1024 + dim % 32 * 32 + ((o ^ (dim >> 3 & 1)) << 4) + 2 * j;
                 acc[d][k] = fmaf(pr, T::up(*(const uint16_t*)vp), acc[d][k]);
               }
           }
