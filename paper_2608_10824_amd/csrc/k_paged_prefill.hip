@@ -20,10 +20,10 @@
 // waits for all LDS reads where it needs one (5% slower), and a page's address
 // stays in scalar registers.
 //
-// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 533 us, 1032 TFLOP/s of
-// the products that rows see, 85% of a large matrix product's rate (matrix cores busy 51%,
-// vector units 45% of the time: the softmax costs as much as the products, and
-// the two take turns); heads of 64 312 us, 881 TFLOP/s; 4 prompts of 1000 rows 58 us.
+// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 527 us, 1044 TFLOP/s of
+// the products that rows see, 86% of a large matrix product's rate (matrix cores busy 52%,
+// vector units 46% of the time: the softmax costs as much as the products, and
+// the two take turns); heads of 64 307 us, 896 TFLOP/s; 4 prompts of 1000 rows 58 us.
 #include "gvc_paged_rows.h"
 #include "gvc_sync.h"
 

@@ -18,9 +18,9 @@ from . import gvc
 
 _DTYPES = {torch.bfloat16: gvc.BF16, torch.float16: gvc.FP16}
 
-# Descriptors and workspace sizes by shape: making one costs more than a short
-# call's other checks together.
-_descs, _sizes = {}, {}
+# Descriptors (by query heads) and workspace sizes (by a call's numbers) of each
+# shape of cache: making one costs more than a short call's other checks together.
+_shapes = {}
 _KEPT = 4096
 
 
@@ -66,6 +66,7 @@ class PagedCache:
         self.n_kv_heads, self.head_dim = kv, dh
         self._dtype, self._index = dtype, index
         self._shape = (dtype, *shape, self.n_seqs, columns)
+        self._descs, self._sizes = _kept(_shapes, self._shape, lambda: ({}, {}))
 
     @property
     def device(self):
@@ -167,19 +168,22 @@ class PagedCache:
     # ---- argument checks and marshalling
     def _desc(self, heads):
         """The descriptor for this many query heads."""
-        def make():
+        desc = self._descs.get(heads)
+        if desc is None:
             dtype, n_pages, kv, page, dh, n_seqs, columns = self._shape
-            return gvc.PagedDesc(_DTYPES[dtype], heads, kv, dh, page, n_pages, n_seqs, columns)
-        return _kept(_descs, (self._shape, heads), make)
+            desc = gvc.PagedDesc(_DTYPES[dtype], heads, kv, dh, page, n_pages, n_seqs, columns)
+            self._descs[heads] = desc
+        return desc
 
     def _workspace(self, desc, heads, prefill, n, window, sinks):
         """Workspace for one call (None: none needed), from the caching
         allocator: it is this call's alone on any stream and in any graph."""
-        def make():
+        key = (heads, prefill, n, window, sinks)
+        size = self._sizes.get(key)
+        if size is None:
             if not (-2 ** 31 <= window < 2 ** 31 and -2 ** 31 <= sinks < 2 ** 31):   # the C call would see other numbers
                 raise ValueError("window and sinks must fit 32 bits")
-            return gvc.paged_workspace(desc, prefill, n, window, sinks)
-        size = _kept(_sizes, (self._shape, heads, prefill, n, window, sinks), make)
+            size = _kept(self._sizes, key, lambda: gvc.paged_workspace(desc, prefill, n, window, sinks))
         return torch.empty(size, dtype=torch.uint8, device=self.k_pages.device) if size else None
 
     def _rows(self, t, name, heads):
@@ -211,8 +215,8 @@ class PagedCache:
         heads = q.shape[1] if q.dim() == 3 else 0
         n, qs = self._rows(q, "q", heads)
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=self._dtype, device=q.device)
-            return heads, n, qs, out, heads * self.head_dim
+            # contiguous, whatever q's strides
+            return heads, n, qs, torch.empty_like(q, memory_format=torch.contiguous_format), heads * self.head_dim
         m, os = self._rows(out, "the output", heads)
         if m != n:
             raise ValueError("the output must have q's rows")
