@@ -564,15 +564,16 @@ __global__ __launch_bounds__(NT) void k_paged_join(const PagedAttnArgs a, const 
 }
 
 // Lists of rows come here rather than to the 128-row tiles of the prefill
-// kernel where there is little to do in all (8 rows of 32 heads over 2000 slots:
-// 16 us against 18; 148 over 276: 10 against 24; 128 over 2000: 42 against 29),
-// or few sequences have one tile of rows each (2 rows of 32 heads on 8, 8
-// sequences of 8000 slots: 58 us against 65; 64 such sequences of 600: 48
-// against 38).
+// kernel where there is little to do in all (276 rows over 276 slots, 32 heads: 13.1 us
+// against 17.8; 300 over 300, 32 heads on 8: 13.8 against 17.1; 8 over 16000: 23.7
+// against 28.7; on the other side of the bound 128 over 2000: 28.9 against 25.6, 16
+// lists of 148 over 276, 32 heads: 77 against 37), or few sequences have one
+// tile of rows each (2 rows of 32 heads on 8, 8 sequences of 8000 slots: 56 us
+// against 65; 64 such sequences of 600 slots: the same).
 bool paged_few_rows(const PagedPool& p, int n_rows, int window, int n_sinks) {
   const int64_t slots = (int64_t)p.max_pages << p.page_shift, seen = (int64_t)window + n_sinks + 64;
   const int64_t most = window && seen < slots ? seen : slots;
-  if ((int64_t)n_rows * p.H * most <= 1 << 21) return true;
+  if ((int64_t)n_rows * p.H * most <= 1 << 22) return true;
   return (int64_t)n_rows * (p.H / p.Hk) <= (int64_t)p.n_seqs * 16 && p.n_seqs * p.Hk <= 128;
 }
 

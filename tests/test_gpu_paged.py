@@ -366,7 +366,7 @@ def test_prefill_rows_that_see_nothing_and_rows_of_no_sequence():
     pool.expect(out[2:], q[2:], [1] * 3 + [2] * 5, [9] * 8)
 
 
-@pytest.mark.parametrize("rows,length", [(10, 50), (10, 3000), (300, 3000)])
+@pytest.mark.parametrize("rows,length", [(10, 50), (10, 3000), (300, 3000), (400, 3000)])
 def test_prefill_with_bounds_that_fall(rows, length):
     """Bounds have to rise; where they do not, no row outside them is touched (nor any other memory)."""
     pool = Pool(26, "bf16", 2, 64, 16, [length] * 4)
@@ -447,13 +447,13 @@ def _tiled(pool, rows, heads, window=0, sinks=0):
     """The calls below are of this kind (what sends them there is in k_paged_decode.hip)."""
     slots = pool.table.shape[1] * pool.page
     most = min(window + sinks + 64, slots) if window else slots
-    assert rows * heads * most > 1 << 21 and rows * heads // pool.kv > 16 * pool.table.shape[0]
+    assert rows * heads * most > 1 << 22 and rows * heads // pool.kv > 16 * pool.table.shape[0]
 
 
 @pytest.mark.parametrize("t", ["bf16", "fp16"])
-@pytest.mark.parametrize("heads,kv,dh,page,columns", [(28, 4, 128, 16, 0), (40, 1, 64, 32, 0), (32, 16, 64, 128, 0),
-                                                      (27, 1, 128, 64, 0), (6, 2, 128, 16, 90), (5, 1, 64, 128, 12),
-                                                      (4, 4, 64, 16, 180)])
+@pytest.mark.parametrize("heads,kv,dh,page,columns", [(56, 8, 128, 16, 0), (64, 1, 64, 32, 0), (64, 32, 64, 128, 0),
+                                                      (53, 1, 128, 64, 0), (6, 2, 128, 16, 195), (5, 1, 64, 128, 26),
+                                                      (4, 4, 64, 16, 200)])
 def test_tiles_of_ragged_rows(t, heads, kv, dh, page, columns):
     """Whole prompts, one row, no row, chunks behind a cached prefix, rows with
     gaps, rows in falling order; tables that hold the lengths alone, and such
@@ -464,11 +464,12 @@ def test_tiles_of_ragged_rows(t, heads, kv, dh, page, columns):
     _ragged(pool, heads, rows)
 
 
-@pytest.mark.parametrize("t,dh,page,heads,kv", [("bf16", 64, 16, 128, 2), ("fp16", 128, 64, 120, 1)])
+@pytest.mark.parametrize("t,dh,page,kv", [("bf16", 64, 16, 2), ("fp16", 128, 64, 1)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (9, 4), (64, 0), (31, 33), (130, 5), (64, 200), (300, 2)])
-def test_tiles_with_window_and_sinks(t, dh, page, heads, kv, window, sinks):
+def test_tiles_with_window_and_sinks(t, dh, page, kv, window, sinks):
     pool = Pool(52, t, kv, dh, page, [333, 20, 180])
     rows = [range(140, 333), range(20), range(0, 180, 3)]
+    heads = ((1 << 22) // (273 * kv * min(window + sinks + 64, 300)) + 1) * kv
     _tiled(pool, 273, heads, window, sinks)
     _ragged(pool, heads, rows, window, sinks)
 
@@ -478,21 +479,21 @@ def test_tiles_over_many_slots(t, dh, page):
     """Few tiles over thousands of slots, split and joined: in up to sixteen
     parts and in more, with and without a window, and rows that see few of them."""
     pool = Pool(53, t, 1, dh, page, [5100])
-    _tiled(pool, 41, 12)
-    _ragged(pool, 12, [[5099, 0, 300] + list(range(5062, 5100))])
-    _tiled(pool, 90, 16, 1500, 70)
-    _ragged(pool, 16, [range(5010, 5100)], 1500, 70)
+    _tiled(pool, 41, 21)
+    _ragged(pool, 21, [[5099, 0, 300] + list(range(5062, 5100))])
+    _tiled(pool, 90, 30, 1500, 70)
+    _ragged(pool, 30, [range(5010, 5100)], 1500, 70)
     pool = Pool(54, t, 2, dh, page, [2000, 130, 900])
     rows = [range(1900, 2000), range(130), [899]]
-    _tiled(pool, 231, 6)
-    _ragged(pool, 6, rows)
+    _tiled(pool, 231, 10)
+    _ragged(pool, 10, rows)
 
 
 @pytest.mark.parametrize("columns", [0, 200])
 def test_tiles_where_rows_see_nothing_or_see_each_other(columns):
     """Empty rows among others and whole tiles of them, an action block whose
     rows give the block's last slot, rows of no sequence before and behind."""
-    heads = 48 if columns == 0 else 6
+    heads = 80 if columns == 0 else 6
     pool = Pool(55, "bf16", 2, 64, 16, [256, 60], extra_columns=columns)
     lasts = [5] * 7 + [-1, 3, -1, 49] + list(range(90)) + [99] * 30 + [-1] * 90 + [7, -9, 59] + [8] * 6
     n = len(lasts)
@@ -506,7 +507,7 @@ def test_tiles_where_rows_see_nothing_or_see_each_other(columns):
 
 @pytest.mark.parametrize("columns", [0, 200])
 def test_tiles_with_pages_that_do_not_exist(columns):
-    heads = 48 if columns == 0 else 6
+    heads = 72 if columns == 0 else 6
     pool = Pool(56, "fp16", 1, 64, 16, [256, 128, 64], extra_columns=columns)
     c = pool.cache
     for s, col, to in ((0, 0, -1), (0, 3, c.k_pages.shape[0]), (0, 9, -2 ** 31), (1, 2, 2 ** 31 - 1), (2, 0, -7),
@@ -523,8 +524,8 @@ def test_tiles_with_pages_that_do_not_exist(columns):
     pool.expect(out, q, [0] * 250, [last] * 250)
 
 
-@pytest.mark.parametrize("t,heads,columns,window,sinks", [("bf16", 48, 0, 0, 0), ("fp16", 48, 0, 0, 0), ("bf16", 4, 180, 0, 0),
-                                                          ("fp16", 104, 0, 40, 4), ("bf16", 104, 200, 40, 4)])
+@pytest.mark.parametrize("t,heads,columns,window,sinks", [("bf16", 72, 0, 0, 0), ("fp16", 72, 0, 0, 0), ("bf16", 6, 180, 0, 0),
+                                                          ("fp16", 156, 0, 40, 4), ("bf16", 156, 200, 40, 4)])
 @pytest.mark.parametrize("dh", [64, 128])
 def test_tiles_keep_nan_and_infinities_with_the_rows_that_see_them(t, heads, columns, window, sinks, dh):
     pool = Pool(57, t, 2, dh, 16, [256], extra_columns=columns)
@@ -547,18 +548,18 @@ def test_tiles_of_steep_scores(t):
     pool = Pool(58, t, 1, 64, 16, [256])
     for j in range(256):
         pool.cache.k_pages[pool.table[0, j // 16], 0, j % 16] *= (j % 50) / 10
-    _tiled(pool, 256, 40)
-    _ragged(pool, 40, [range(256)], scale=4.0)
+    _tiled(pool, 256, 72)
+    _ragged(pool, 72, [range(256)], scale=4.0)
 
 
 def test_tiles_strides_scale_and_out():
     pool = Pool(59, "bf16", 2, 128, 32, [256])
-    wide = pool.rows(256, 50)
-    q = wide[:, 4:44]
-    held = torch.full((256, 42, 128), 3.0, dtype=torch.bfloat16, device=DEV)
-    _tiled(pool, 256, 40)
-    out = pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3, out=held[:, 1:41])
-    assert (held[:, 0] == 3).all() and (held[:, 41] == 3).all()
+    wide = pool.rows(256, 70)
+    q = wide[:, 4:64]
+    held = torch.full((256, 62, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+    _tiled(pool, 256, 60)
+    out = pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3, out=held[:, 1:61])
+    assert (held[:, 0] == 3).all() and (held[:, 61] == 3).all()
     pool.expect(out, q, [0] * 256, range(256), scale=0.3)
 
 
@@ -788,7 +789,7 @@ def test_pool_over_four_gib():
 def test_outputs_in_place_of_their_inputs():
     """q_out or out may be q itself: rotation, unsplit and split decodes and
     lists of rows of both kinds give the same bits."""
-    pool = Pool(37, "bf16", 2, 64, 16, [1500, 40, 0])
+    pool = Pool(37, "bf16", 2, 64, 16, [1500, 40, 0], extra_columns=20)
     c, n = pool.cache, 300
     x = pool.rows(n, 12)
     seq, slot = pool.ints([0] * n), pool.ints(range(1200, 1500))
@@ -806,8 +807,8 @@ def test_outputs_in_place_of_their_inputs():
     want = c.prefill(q, slot, pool.ints([0, n, n, n]))
     assert torch.equal(c.prefill(q, slot, pool.ints([0, n, n, n]), out=q), want)
     pool = Pool(38, "fp16", 1, 128, 32, [256], extra_columns=0)
-    q, slot = pool.rows(256, 40), pool.ints(range(256))
-    _tiled(pool, 256, 40)
+    q, slot = pool.rows(256, 72), pool.ints(range(256))
+    _tiled(pool, 256, 72)
     want = pool.cache.prefill(q, slot, pool.ints([0, 256]))
     assert torch.equal(pool.cache.prefill(q, slot, pool.ints([0, 256]), out=q), want)
 
