@@ -9,6 +9,14 @@ namespace gvc {
 // v, which is the same in every lane, as a scalar: loops and branches on it stay scalar.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// The lowest n of eight bits, for any n.
+__device__ __forceinline__ uint32_t first8(int n) { return (1u << min(max(n, 0), 8)) - 1; }
+// x if bit i is set, else -infinity: two instructions and no condition register.
+__device__ __forceinline__ float seen_score(uint32_t bits, int i, float x) {
+  const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, i, 1);
+  return __uint_as_float((__float_as_uint(x) & keep) | (0xff800000u & ~keep));
+}
+
 // A sequence's first row and number of virtual rows, and the last slot that its
 // last row sees.
 struct SeqRows {

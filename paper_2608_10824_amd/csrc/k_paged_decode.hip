@@ -323,17 +323,13 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
     if (full) {
       any = true;
     } else {
-      seen = 0;
-      unsigned some = 0;
+      const int j = j0 + 8 * g;
+      const unsigned sinks = first8(a.n_sinks - j), page = okv ? ~0u : 0u;
+      seen = first8(last + 1 - j) & (~first8(lo + 1 - j) | sinks) & page;
+      // one token: all rows see the same
+      const unsigned some = ROWS ? first8(hi_some + 1 - j) & (~first8(lo_some + 1 - j) | sinks) & page : seen;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int j = j0 + 8 * g + u;
-        const bool in = okv & (j <= last) & ((j > lo) | (j < a.n_sinks));
-        x[u] = in ? x[u] : -INFINITY;
-        seen |= (unsigned)in << u;
-        if (ROWS) some |= (unsigned)(okv & (j <= hi_some) & ((j > lo_some) | (j < a.n_sinks))) << u;
-      }
-      if (!ROWS) some = seen;   // one token: all rows see the same
+      for (int u = 0; u < 8; ++u) x[u] = seen_score(seen, u, x[u]);
       any |= seen != 0;
       pu32x4 keep;
 #pragma unroll

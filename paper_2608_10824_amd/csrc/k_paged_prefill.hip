@@ -39,9 +39,6 @@ constexpr int kPreMaxParts = kPreUnits;
 // Kinds of instructions for sched_group_barrier.
 constexpr int kMfma = 0x8, kDsRead = 0x100;
 
-// The lowest n of eight bits, for any n.
-__device__ __forceinline__ uint32_t first8(int n) { return (1u << min(max(n, 0), 8)) - 1; }
-
 // The tile of virtual rows that a workgroup takes.
 struct RowTile {
   int seq, first, begin, rows;   // sequence (-1: none), the tile's first virtual row, the sequence's first row, its virtual rows
@@ -245,7 +242,7 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
                 << (8 * g);
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = seen & (1u << i) ? s[i >> 4][i & 15] : -INFINITY;
+      for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = seen_score(seen, i, s[i >> 4][i & 15]);
       any |= seen != 0;
     }
     float top = -INFINITY;
