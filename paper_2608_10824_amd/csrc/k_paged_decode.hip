@@ -18,7 +18,7 @@
 // result does not depend on which one that is; where there may be more than
 // kFuseChunks of them, by a second launch with a workgroup for each row.
 //
-// Measured (bf16, 128 to a head): one sequence of 282 slots, 32 heads, 7.3 us (a
+// Measured (bf16, 128 to a head): one sequence of 282 slots, 32 heads, 7.1 us (a
 // chain of launch, table, keys, values: 4.8 us for one slot); of 131072, 32 heads on
 // 8, 103.5 us, 5.2 TB/s; 16 sequences of 500 to 900 slots, 32 heads, 32.5 us, 4.5
 // TB/s; 64 of 5 to 16384 slots, 64 heads on 8, fp16, 123 us, 4.5 TB/s.
