@@ -188,10 +188,10 @@ __device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int G, int num
 // head][column][DH + 4] floats: maximum, sum, whether a slot was seen, nothing,
 // output.  Columns: G, at most 16, for one row per sequence, else 16.
 //
-// A unit that is done sets its flag to the call's tag, and when the store has
-// come through reads the flags of its row tile's units: the last one finds them
-// all set (two may, and write the same output), and clears them.  A tag is no
-// other call's (see paged_tag), so what memory holds before does not matter, nor how
+// A unit that is done sets its flag to the call's tag, and when that has come
+// through reads the flags of its row tile's units: the last one finds them all
+// set (two may, and write the same output), and clears them.  A tag is no other
+// call's (see paged_tag), so what memory holds before does not matter, nor how
 // often a captured call is replayed.  (A counter needs read-modify-writes of one
 // address by all units, about 1 us each: 16 chunks took 13 us longer.)
 __host__ __device__ __forceinline__ int64_t flag_bytes(int64_t units) { return (units * 8 + 15) / 16 * 16; }
@@ -506,7 +506,10 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
   int* join = (int*)lds;
   if (wv == 0) {
     uint64_t* flags = (uint64_t*)work;
-    if (lane == 0) put(flags + blockIdx.x, a.tag);
+    if (lane == 0) {   // an exchange whose answer is there has been seen by every XCD
+      const uint64_t held = __hip_atomic_exchange(flags + blockIdx.x, a.tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("" ::"v"(held));
+    }
     stores_done();
     uint64_t* theirs = flags + (first + (int64_t)min(lane, unit.count - 1) * row_tiles) * p.Hk + kvh;   // chunk `lane`'s
     const bool all = __all(get(theirs) == a.tag);
