@@ -43,7 +43,13 @@ int32_t device(hipError_t e) noexcept {
 }
 
 constexpr int64_t kMaxSlots = 1 << 30;
-constexpr int64_t kMaxHeadRows = 1 << 28;   // 16 threads each: a launch has less than 2^32
+// A launch has less than 2^32 threads.  Attention takes two to a row and head and
+// 256 to a sequence and key-value head, or at most 2^30 (short lists, and one row to
+// each of 4096 sequences).  Append takes 64 to a row and another 2^18 at most (a wave of
+// queries and keys, more only for fewer than 4096 rows) and 8 to a row and key-value
+// head (values): with heads counted as five at least, under 0.91 x 2^32.
+constexpr int64_t kMaxHeadRows = 1 << 28;
+constexpr int kAppendLeastHeads = 5;
 
 // nullptr, or what is wrong with d
 const char* bad_desc(const gvc_paged_desc* d) noexcept {
@@ -167,8 +173,8 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   if (n % 4 || 2 * n > d.head_dim) return fail("the sum of pairs must be a multiple of 4, at most head_dim / 2");
   if (!(rope->theta > 0.f) || !std::isfinite(rope->theta)) return fail("theta must be positive and finite");
   if (!(rope->rms_eps >= 0.f)) return fail("rms_eps must be >= 0");
-  if (n_rows < 0 || (int64_t)n_rows * (d.n_heads + 2 * d.n_kv_heads) >= kMaxHeadRows)
-    return fail("n_rows must be >= 0, and n_rows * (n_heads + 2 n_kv_heads) below 2^28");
+  if (n_rows < 0 || (int64_t)n_rows * std::max(d.n_heads + 2 * d.n_kv_heads, kAppendLeastHeads) >= kMaxHeadRows)
+    return fail("n_rows must be >= 0, and n_rows * max(n_heads + 2 n_kv_heads, 5) below 2^28");
   if ((q == nullptr) != (q_out == nullptr) && n_rows) return fail("q and q_out come together");
   if (n_rows == 0) return GVC_OK;
   if (!row_seq || !row_slot || !k_pages || !v_pages || !page_table) return fail("null argument");

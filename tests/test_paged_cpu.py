@@ -83,6 +83,13 @@ def test_bad_append_refused(kw):
     _refused(_append, _desc(), _rope(), **kw)
 
 
+@pytest.mark.parametrize("heads,kv,n", [(1, 1, 1 << 26), (1, 1, 53687092), (2, 1, (1 << 26) - 1), (2, 1, 53687092)])
+def test_more_rows_than_a_launch_has_threads_refused(heads, kv, n):
+    """n (heads + 2 kv) is below 2^28, but a row takes 64 threads and its values 8: 2^32 are the most."""
+    assert n * (heads + 2 * kv) < 1 << 28
+    _refused(_append, _desc(n_heads=heads, n_kv_heads=kv), _rope(), n=n, qs=128)
+
+
 @pytest.mark.parametrize("call", [_decode, _prefill])
 @pytest.mark.parametrize("kw", [dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
                                 dict(window=-1), dict(sinks=-1), dict(q=None), dict(kp=None), dict(vp=None),
