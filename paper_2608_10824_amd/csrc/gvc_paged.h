@@ -85,8 +85,17 @@ typedef uint16_t pu16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t pu16x8 __attribute__((ext_vector_type(8)));
 
 // The running maximum may lag behind the true one by 2^kPagedLazy before output
-// and sum are rescaled: a probability is at most 2^kPagedLazy, far from overflow.
+// and sum are rescaled: a probability is at most 2^kPagedLazy.
 constexpr float kPagedLazy = 8.f;
+
+// Outputs are summed before they are divided by the sum of the probabilities, so in
+// bf16, whose values reach 2^128, a sum may overflow where the output is finite.  A
+// wave whose sums reach kPagedLarge, or are not finite, does them again relative to
+// 2^spare_bits above its maximum: the probabilities of its slots then add up to at
+// most 2^-13.  Either way a wave's sums are below 2^115, and the 4 x 1026 of them that
+// are joined at most below 2^128.  (In such a wave products of a probability and a
+// value under 2^-126 + spare_bits are lost.)
+constexpr float kPagedLarge = 0x1p115f;
 
 // The two 16-bit types.  Conversions to 16 bits round to nearest even.  What is
 // rounded to them, once each: a rotated query or key (the pages hold 16 bits), a
@@ -105,6 +114,7 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
   static constexpr float kShift = 0.f;   // see Fp16
+  static constexpr bool kOverflows = true;
 };
 struct Fp16 {
   typedef _Float16 elem;
@@ -122,6 +132,8 @@ struct Fp16 {
   // scaled by 2^kShift, sum and output alike, and still fit: a probability is
   // at most 2^kPagedLazy before scaling.
   static constexpr float kShift = 6.f;
+  // 2^30 slots at most, probabilities of 2^14, values of 2^16: sums are below 2^60.
+  static constexpr bool kOverflows = false;
 };
 
 template <class T>
@@ -129,6 +141,9 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const pf32x2 f = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, typename T::x2));
 }
+
+// For n tiles of 2^tile_log slots.
+__device__ __forceinline__ int spare_bits(int n, int tile_log) { return 13 + tile_log + 32 - __builtin_clz(max(n, 1)); }
 
 // The largest over the four 16-lane rows of a wave, lane by lane.
 __device__ __forceinline__ float rows_max(float v) {

@@ -219,6 +219,17 @@ __device__ __forceinline__ pf32x4 get4(const float* from) {
 // Waits until this wave's stores are where every XCD reads them.
 __device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// At least as large as every |acc|, NaN where one is NaN.
+template <int N>
+__device__ __forceinline__ float magnitude(const pf32x4 (&acc)[N]) {
+  pf32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += fabsf(acc[c][i]);
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
 template <class T, int DH, bool ROWS>
 __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs a, char* work, int64_t units, bool fused,
                                                               int least_chunk) {
@@ -240,11 +251,16 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
   const int in_page = (1 << p.page_shift) - 1;
   const int row = row_of(min(col, qs - 1));
   pu32x4 qf[NK];
+  auto load_q = [&]() {
+    const uint16_t* q = a.q;
+    asm volatile("" : "+s"(q));   // an address of its own: the second call loads, and keeps no registers until then
 #pragma unroll
-  for (int kk = 0; kk < NK; ++kk) {
-    qf[kk] = *(const pu32x4*)(a.q + row * a.q_stride + head_of(min(col, qs - 1)) * DH + g * 8 + kk * 32);
-    if (col >= qs) qf[kk] = pu32x4{0, 0, 0, 0};
-  }
+    for (int kk = 0; kk < NK; ++kk) {
+      qf[kk] = *(const pu32x4*)(q + row * a.q_stride + head_of(min(col, qs - 1)) * DH + g * 8 + kk * 32);
+      if (col >= qs) qf[kk] = pu32x4{0, 0, 0, 0};
+    }
+  };
+  load_q();
   // The last slot of the lane's row, and what the tile's rows see: slots in
   // (lo_some, hi_some] (or below the sinks) some row, in (lo_all, hi_all] every row.
   int last = unit.rows.last, hi_some = last, hi_all = last, least = last;
@@ -373,21 +389,21 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
     t = next;
     load_v(t, more);
   }
-  // Where the output is not finite the wave does it again, slowly: a slot that
-  // only some rows of the tile see is added to those alone, so that NaN and
-  // infinities in its values stay with them.
-  if (ROWS) {
-    bool bad = false;
-#pragma unroll
-    for (int c = 0; c < NO; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= !(fabsf(acc[c][i]) < INFINITY);
-    if (__any(bad)) {
+  // Where a sum is not finite, or too large to be joined with others (kPagedLarge),
+  // the wave does its tiles again, slowly, with the true maximum and the spare bits.
+  // In lists of rows a slot that only some rows of the tile see is then added to those
+  // alone, by its unrounded probability, so that NaN and infinities in its values
+  // stay with them; with one token all rows see the same.  (The test takes 0.1 to 0.25 us
+  // of a call; out of the way and with q loaded anew: registers that it would keep made
+  // the wave wait for the last round's unused loads, 0.5 us.)
+  if (ROWS || T::kOverflows) {
+    if (__builtin_expect(__any((col < qs) & !(magnitude(acc) < kPagedLarge)), 0)) {
+      const float spare = (float)spare_bits(t_end - t0, 5);
 #pragma unroll
       for (int c = 0; c < NO; ++c) acc[c] = pf32x4{0, 0, 0, 0};
       m = -INFINITY;
       l = 0.f;
-      shift = T::kShift;
+      load_q();
       load_ids(0);
 #pragma unroll 1
       for (int t = t0, n = 0; t < t_end; t += NW, ++n) {
@@ -412,7 +428,7 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
         const float mn = fmaxf(m, rows_max(top * a.scale_log2e)), nb = mn == -INFINITY ? 0.f : mn;
         const float f = __builtin_amdgcn_exp2f(m - nb);
         m = mn;
-        shift = T::kShift - nb;
+        shift = T::kShift - nb - spare;
         l *= f;
 #pragma unroll
         for (int c = 0; c < NO; ++c) acc[c] *= f;
@@ -421,22 +437,34 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
           x[u] = __builtin_amdgcn_exp2f(fmaf(x[u], a.scale_log2e, shift));
           l += x[u];
         }
+        if constexpr (!ROWS) {
+          load_v(t, true);
+          pu32x4 keep;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            keep[w] = ((seen >> (2 * w)) & 1 ? 0xffffu : 0u) | ((seen >> (2 * w + 1)) & 1 ? 0xffff0000u : 0u);
+          const pu32x4 pf = {pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])};
+#pragma unroll
+          for (int c = 0; c < NO; ++c) acc[c] = T::mfma16(vf[c] & keep, pf, acc[c]);
+        } else {
 #pragma unroll 1
-        for (int o = 0; o < 4; ++o) {   // the slots of lane group o
-          const unsigned bits = (unsigned)__shfl((int)seen, 16 * o + col);
-          const int64_t page = o < 2 ? max(id0, 0) : max(id1, 0);
-          const uint16_t* vp = p.v + (((page * p.Hk + kvh) * DH + 4 * g) << p.page_shift) + ((j0 + 8 * o) & in_page);
+          for (int o = 0; o < 4; ++o) {   // the slots of lane group o
+            const unsigned bits = (unsigned)__shfl((int)seen, 16 * o + col);
+            const int64_t page = o < 2 ? max(id0, 0) : max(id1, 0);
+            const uint16_t* vp = p.v + (((page * p.Hk + kvh) * DH + 4 * g) << p.page_shift) + ((j0 + 8 * o) & in_page);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float pr = T::up((uint16_t)pack2<T>(__shfl(x[u], 16 * o + col), 0.f));
-            if ((bits >> u) & 1)
+            for (int u = 0; u < 8; ++u) {
+              const float pr = __shfl(x[u], 16 * o + col);
+              if ((bits >> u) & 1)
 #pragma unroll
-              for (int c = 0; c < NO; ++c)
+                for (int c = 0; c < NO; ++c)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[c][i] = fmaf(pr, T::up(vp[((16 * c + i) << p.page_shift) + u]), acc[c][i]);
+                  for (int i = 0; i < 4; ++i) acc[c][i] = fmaf(pr, T::up(vp[((16 * c + i) << p.page_shift) + u]), acc[c][i]);
+            }
           }
         }
       }
+      m += spare;
     }
   }
 

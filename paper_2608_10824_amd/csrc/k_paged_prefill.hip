@@ -284,14 +284,15 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
       pf = next;
     }
   }
-  // Where an output is not finite the workgroup does its rows again, slowly: a
-  // slot that only some rows of a wave see is added to those alone, so that NaN
-  // and infinities in its values stay with them.
+  // Where a sum is not finite, or too large to be joined with others (kPagedLarge),
+  // the workgroup does its rows again, slowly, with the true maximum and the spare
+  // bits: a slot that only some rows of a wave see is added to those alone, by its
+  // unrounded probability, so that NaN and infinities in its values stay with them.
   bool bad = false;
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) bad |= !(fabsf(acc[d][i]) < INFINITY);
+    for (int i = 0; i < 16; ++i) bad |= !(fabsf(acc[d][i]) < kPagedLarge);
   const int wave_bad = __any(bad && live);
   __syncthreads();   // LDS is free
   if (lane == 0) shared_rows[wv] = wave_bad;
@@ -301,6 +302,7 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
   for (int w = 0; w < kPreWaves; ++w) again |= shared_rows[w] != 0;
   __syncthreads();
   if (again) {
+    const float spare = (float)spare_bits(t_end - t_begin, 6);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -346,11 +348,11 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int i = 8 * m + j;
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, T::kShift - nb));
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], a.scale_log2e, T::kShift - nb - spare));
           l_run += x;
 #pragma unroll 1
           for (int o = 0; o < 2; ++o) {   // slot 16 m + 8 o + j, of the lanes with half == o
-            const float pr = T::up((uint16_t)pack2<T>(__shfl(x, 32 * o + r32), 0.f));
+            const float pr = __shfl(x, 32 * o + r32);
             if (!(((unsigned)__shfl((int)seen, 32 * o + r32) >> i) & 1)) continue;
 #pragma unroll
             for (int d = 0; d < ND; ++d)
@@ -364,6 +366,7 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
         }
       __syncthreads();
     }
+    m_run += spare;
   }
 
   const float l = l_run + __shfl_xor(l_run, 32);

@@ -845,3 +845,35 @@ def test_wrapper_refusals():
               lambda: c.append(q, k, v, two, two, rope_pairs=(33,)), lambda: c.append(q, k, v, two, two, rms_eps=-1.0)):
         with pytest.raises(gvc.GvcError):
             f()
+
+
+# ------------------------------------------- values near the end of the type's range
+def _large(pool, power):
+    """The pool's values up to 2^(power + 2), all of one sign: their sums before the division are larger."""
+    pool.cache.v_pages.abs_().clamp_(max=4).mul_(2.0 ** power)
+
+
+@pytest.mark.parametrize("power", [90, 114, 121, 125])
+def test_outputs_are_finite_where_sums_overflow(power):
+    """bf16 values to 2^127: decode (split and not, with a window) and lists of few rows give
+    the finite outputs of their formulas."""
+    lengths = [1, 40, 700, 3000, 0]
+    pool = Pool(63, "bf16", 2, 64, 16, lengths)
+    _large(pool, power)
+    q = pool.rows(5, 8, 2.0)
+    pool.expect(pool.cache.decode(q, pool.ints(lengths)), q, range(5), [n - 1 for n in lengths])
+    pool.expect(pool.cache.decode(q, pool.ints(lengths), window=300, sinks=20), q, range(5), [n - 1 for n in lengths], 300, 20)
+    _ragged(pool, 8, [[0], range(40), [699, 3], [2999], []])
+    pool = Pool(64, "bf16", 1, 128, 32, [300, 33], extra_columns=0)
+    _large(pool, power)
+    q = pool.rows(2, 20, 2.0)
+    pool.expect(pool.cache.decode(q, pool.ints([300, 33])), q, range(2), [299, 32])
+
+
+@pytest.mark.parametrize("power", [90, 114, 121, 125])
+@pytest.mark.parametrize("dh,heads,columns", [(64, 72, 0), (128, 72, 0), (64, 6, 200), (128, 6, 200)])
+def test_tiles_are_finite_where_sums_overflow(power, dh, heads, columns):
+    pool = Pool(65, "bf16", 2, dh, 16, [256], extra_columns=columns)
+    _large(pool, power)
+    _tiled(pool, 256, heads)
+    _ragged(pool, heads, [range(256)])
