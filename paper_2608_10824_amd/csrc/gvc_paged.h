@@ -115,6 +115,7 @@ struct Bf16 {
   }
   static constexpr float kShift = 0.f;   // see Fp16
   static constexpr bool kOverflows = true;
+  static constexpr float kMax = 0x1.fep127f;   // the largest value
 };
 struct Fp16 {
   typedef _Float16 elem;
@@ -134,12 +135,22 @@ struct Fp16 {
   static constexpr float kShift = 6.f;
   // 2^30 slots at most, probabilities of 2^14, values of 2^16: sums are below 2^60.
   static constexpr bool kOverflows = false;
+  static constexpr float kMax = 65504.f;
 };
 
 template <class T>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const pf32x2 f = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, typename T::x2));
+}
+
+// Four outputs.  An average of values is not larger than the largest of them, but the
+// rounded probabilities can carry it there: a finite one stays within the type.
+template <class T>
+__device__ __forceinline__ pu32x2 pack_out(pf32x4 o) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = fabsf(o[i]) < INFINITY ? fminf(fmaxf(o[i], -T::kMax), T::kMax) : o[i];
+  return {pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
 }
 
 // For n tiles of 2^tile_log slots.

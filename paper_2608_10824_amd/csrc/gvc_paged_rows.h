@@ -111,7 +111,7 @@ __device__ __forceinline__ void join_row(const float* from, int64_t step, int n,
   const float inv = 1.f / l;
 #pragma unroll
   for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-  *(pu32x2*)(out + 4 * d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+  *(pu32x2*)(out + 4 * d) = pack_out<T>(o);
 }
 
 }  // namespace gvc

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
       const float inv = 1.f / ll;
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-      *(pu32x2*)(a.out + row_of(q) * a.out_stride + head_of(q) * DH + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+      *(pu32x2*)(a.out + row_of(q) * a.out_stride + head_of(q) * DH + d) = pack_out<T>(o);
     } else {
       float* to = parts + ((int64_t)blockIdx.x * columns(ROWS, G) + q) * row_len;
       const pf32x4 stat = {top, ll, saw, 0.f};
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(NW * 64, 3) void k_paged_decode(const PagedAttnArgs
     const float inv = 1.f / ll;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-    *(pu32x2*)(a.out + row_of(q) * a.out_stride + head_of(q) * DH + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+    *(pu32x2*)(a.out + row_of(q) * a.out_stride + head_of(q) * DH + d) = pack_out<T>(o);
   }
 }
 

@@ -382,10 +382,10 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        float y[4];
+        pf32x4 y;
 #pragma unroll
         for (int k = 0; k < 4; ++k) y[k] = any ? acc[d][i + k] * inv : 0.f;
-        *(pu32x2*)(o + 32 * d + 2 * i) = pu32x2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
+        *(pu32x2*)(o + 32 * d + 2 * i) = pack_out<T>(y);
       }
   } else {
 #pragma unroll
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256) void k_paged_join_tiles(const PagedAttnArgs a,
     const float inv = 1.f / l;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-    *(pu32x2*)(out + d) = pu32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
+    *(pu32x2*)(out + d) = pack_out<T>(o);
   }
 }
 

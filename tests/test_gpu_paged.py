@@ -877,3 +877,34 @@ def test_tiles_are_finite_where_sums_overflow(power, dh, heads, columns):
     _large(pool, power)
     _tiled(pool, 256, heads)
     _ragged(pool, heads, [range(256)])
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+@pytest.mark.parametrize("form", ["decode", "split decode", "rows", "split rows", "tiles", "split tiles"])
+def test_rounded_probabilities_do_not_carry_an_output_past_the_largest_value(t, form):
+    """Every value is the type's largest, so every output is.  One slot of 32 has the most weight, the others just over
+    half of it, which 16 bits round up by almost u: more than from the largest value half way to the next."""
+    n = 2000 if form.startswith("split") else 350
+    tiles = form.endswith("tiles")
+    pool = Pool(66, t, 1, 64, 16, [n], extra_columns=1)
+    c, big, rows = pool.cache, torch.finfo(TYPES[t]).max, 300 if tiles else 1
+    c.v_pages.copy_(torch.where(c.v_pages.isnan(), c.v_pages, torch.full_like(c.v_pages, big)))
+    c.k_pages.copy_(torch.where(c.k_pages.isnan(), c.k_pages, torch.zeros_like(c.k_pages)))
+    for j in range(n):
+        c.k_pages[pool.table[0, j // 16], 0, j % 16, 0] = -1.0 if j % 32 else 0.0
+    scale = -np.log((1 + 1.1 * _u(t)) / 2)
+    heads = 2 if not tiles else 42 if n < 1000 else 8
+    q = torch.zeros(rows, heads, 64, dtype=TYPES[t], device=DEV)
+    q[:, :, 0] = 1
+    if tiles:
+        _tiled(pool, rows, heads)
+    if form.endswith("decode"):
+        out = c.decode(q, pool.ints([n]), scale=scale)
+    else:
+        out = c.prefill(q, pool.ints([n - 1] * rows), pool.ints([0, rows]), scale=scale)
+    assert (out == big).all()
+    out = c.prefill(-q, pool.ints([n - 1] * rows), pool.ints([0, rows]), scale=scale)
+    assert (out == big).all()
+    c.v_pages[pool.table[0, 0], 0, 7, 3] = float("-inf")   # an infinity in sight stays one
+    out = c.prefill(q, pool.ints([n - 1] * rows), pool.ints([0, rows]), scale=scale)
+    assert (out[:, :, 7] == float("-inf")).all() and (out[:, :, :7] == big).all() and (out[:, :, 8:] == big).all()
