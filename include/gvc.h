@@ -396,7 +396,7 @@ typedef struct gvc_paged_desc {
  * video patch, say).  Dimensions from 2 n on are not rotated. */
 typedef struct gvc_paged_rope {
   int32_t pairs[3];       /* >= 0; their sum n a multiple of 4, 0 <= 2 n <= head_dim */
-  float theta;            /* > 0 */
+  double theta;           /* > 0, within the range of a float; its 64 bits count at far positions */
   float rms_eps;          /* >= 0 */
   const void* q_norm;     /* dev [head_dim] or NULL */
   const void* k_norm;     /* dev [head_dim] or NULL */

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <chrono>
 #include <cmath>
 #include <cstdio>
@@ -171,7 +172,8 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
     n += x;
   }
   if (n % 4 || 2 * n > d.head_dim) return fail("the sum of pairs must be a multiple of 4, at most head_dim / 2");
-  if (!(rope->theta > 0.f) || !std::isfinite(rope->theta)) return fail("theta must be positive and finite");
+  // (a base below a float's range would turn by more than a double can reduce)
+  if (!(rope->theta >= FLT_TRUE_MIN && rope->theta <= FLT_MAX)) return fail("theta must be positive and within a float's range");
   if (!(rope->rms_eps >= 0.f)) return fail("rms_eps must be >= 0");
   if (n_rows < 0 || (int64_t)n_rows * std::max(d.n_heads + 2 * d.n_kv_heads, kAppendLeastHeads) >= kMaxHeadRows)
     return fail("n_rows must be >= 0, and n_rows * max(n_heads + 2 n_kv_heads, 5) below 2^28");
@@ -209,7 +211,7 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   a.end1 = rope->pairs[0] + rope->pairs[1];
   a.eps = rope->rms_eps;
   // theta^(-i/n) / 2 pi by repeated products: off by at most 64 roundings of a double
-  const double step = n ? std::pow((double)rope->theta, -1.0 / (double)n) : 1.0;
+  const double step = n ? std::pow(rope->theta, -1.0 / (double)n) : 1.0;
   double turn = 0.15915494309189533577;
   for (int i = 0; i < n; ++i, turn *= step) a.turns[i] = turn;
   return device(launch_paged_append(a, d.dtype, static_cast<hipStream_t>(stream)));

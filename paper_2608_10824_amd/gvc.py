@@ -74,7 +74,7 @@ class PagedDesc(ctypes.Structure):
 
 
 class PagedRope(ctypes.Structure):
-    _fields_ = [("pairs", ctypes.c_int32 * 3), ("theta", ctypes.c_float), ("rms_eps", ctypes.c_float),
+    _fields_ = [("pairs", ctypes.c_int32 * 3), ("theta", ctypes.c_double), ("rms_eps", ctypes.c_float),
                 ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("position_stride", ctypes.c_int64)]
 

@@ -175,6 +175,13 @@ def test_append_far_positions():
     _append(3, "fp16", 2, 2, 128, 16, [n], [(0, j) for j in range(n)], positions=[far], pairs=(64,), theta=1e6)
 
 
+@pytest.mark.parametrize("theta", [10000 * 8 ** (128 / 126), 1234567.89, 0.7])
+def test_append_far_positions_of_bases_that_fp32_does_not_hold(theta):
+    far = [0, 1, 10 ** 5, 10 ** 7 + 3, 123456789, 2 ** 31 - 1, -2 ** 31]
+    n = len(far)
+    _append(67, "fp16", 2, 2, 128, 16, [n], [(0, j) for j in range(n)], positions=[far], pairs=(64,), theta=theta)
+
+
 def test_append_rows_in_any_order_of_any_run_length():
     r = np.random.default_rng(4)
     every = [(s, j) for s, n in enumerate([50, 33, 0, 129]) for j in range(n)]

@@ -75,6 +75,15 @@ def test_bad_rotation_refused(rope):
     _refused(_append, _desc(), _rope(**rope))
 
 
+def test_the_base_keeps_its_64_bits_within_the_range_of_a_float():
+    base = 10000 * 8 ** (128 / 126)
+    assert _rope(theta=base).theta == base
+    for theta in (1e39, -1e39, 1e-46, 1e-320):
+        _refused(_append, _desc(), _rope(theta=theta))
+    _append(_desc(), _rope(theta=3e38), n=0)
+    _append(_desc(), _rope(theta=1e-38), n=0)
+
+
 @pytest.mark.parametrize("kw", [dict(q=None), dict(o=None), dict(k=None), dict(v=None), dict(row_seq=None),
                                 dict(row_slot=None), dict(kp=None), dict(vp=None), dict(table=None), dict(n=-1),
                                 dict(q=P + 8), dict(k=P + 2), dict(v=P + 4), dict(o=P + 8), dict(qs=516), dict(ks=120),
