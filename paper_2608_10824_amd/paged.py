@@ -4,8 +4,8 @@ A `PagedCache` holds the pages and the page table of one layer; its calls
 append rows to the pages and attend over them (include/gvc.h, "paged cache",
 says what each computes).  PyTorch provides memory and streams; every
 computation is a call into libgvc on the current stream of the cache's GPU,
-asynchronous and fit for capture into a graph.  There is no backward pass:
-tensors that require a gradient are refused.
+asynchronous and fit for capture into a graph.  There are no derivatives:
+tensors that require a gradient, and duals of forward mode, are refused.
 
     cache = PagedCache.empty(n_pages, page_size, n_kv_heads, head_dim, n_seqs, max_pages)
     q = cache.append(q, k, v, row_seq, row_slot, rope_pairs=(16, 24, 24), positions=thw)
@@ -13,6 +13,7 @@ tensors that require a gradient are refused.
     o = cache.decode(q, lengths, window=4096, sinks=4)   # one new token per sequence
 """
 import torch
+from torch.autograd import forward_ad
 
 from . import gvc
 
@@ -31,6 +32,12 @@ def _kept(store, key, make):
             store.clear()
         value = store[key] = make()
     return value
+
+
+def _no_tangents(*tensors):
+    """Refuses duals, whose tangents would be lost (called within a level of forward mode only)."""
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("tensors with a tangent of forward mode: the paged cache has no derivatives")
 
 
 def _address(t):
@@ -56,6 +63,8 @@ class PagedCache:
             raise ValueError("page_table must be int32 [n_seqs][max_pages]")
         if k_pages.requires_grad or v_pages.requires_grad:
             raise ValueError("pages must not require a gradient")
+        if forward_ad._current_level >= 0:
+            _no_tangents(k_pages, v_pages)
         if not (k_pages.is_contiguous() and v_pages.is_contiguous() and page_table.is_contiguous()):
             raise ValueError("pages and page table must be contiguous")
         index = k_pages.get_device()
@@ -87,6 +96,8 @@ class PagedCache:
         rope_pairs: rotated pairs of each axis, at most three (default: the
         whole head on one axis; () rotates nothing); positions: int32
         [axes][rows], default the slots.  q_out may be q itself."""
+        if forward_ad._current_level >= 0:
+            _no_tangents(q, k, v, q_norm, k_norm, q_out)
         kv = self.n_kv_heads
         n, ks = self._rows(k, "k", kv)
         m, vs = self._rows(v, "v", kv)
@@ -123,6 +134,8 @@ class PagedCache:
         """Attention of one token per sequence: q [n_seqs][n_heads][head_dim],
         row s over the first lengths[s] slots (int32; 0: an idle slot of the
         batch, zeros).  scale: default head_dim^-1/2.  out may be q itself."""
+        if forward_ad._current_level >= 0:
+            _no_tangents(q, out)
         heads, n, qs, out, os = self._q_out(q, out)
         if n != self.n_seqs:
             raise ValueError("q must have one row per sequence")
@@ -140,6 +153,8 @@ class PagedCache:
         sees slots up to row_last[r] (int32; -1: none).  Rows of no sequence
         are left as they are in `out` (undefined in a new one), which may be q
         itself."""
+        if forward_ad._current_level >= 0:
+            _no_tangents(q, out)
         heads, n, qs, out, os = self._q_out(q, out)
         self._ints(row_last, "row_last", n)
         self._ints(row_begin, "row_begin", self.n_seqs + 1)

@@ -183,6 +183,40 @@ def test_cache_refuses_host_tensors():
             PagedCache(*a)
 
 
+def _host_cache():
+    """A cache over host memory, which only __init__ refuses: what its calls check comes before the C call."""
+    import torch
+    from paper_2608_10824_amd.paged import PagedCache
+    c = PagedCache.__new__(PagedCache)
+    c.k_pages, c.v_pages = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, 16, dtype=torch.bfloat16)
+    c.page_table = torch.zeros(2, 3, dtype=torch.int32)
+    c.n_seqs, c.n_kv_heads, c.head_dim, c._dtype, c._index = 2, 2, 64, torch.bfloat16, -1
+    c._shape, c._descs, c._sizes = (c._dtype, 4, 2, 16, 64, 2, 3), {}, {}
+    return c
+
+
+def test_forward_mode_duals_are_refused():
+    import torch
+    from torch.autograd import forward_ad
+    from paper_2608_10824_amd.paged import PagedCache
+    c = _host_cache()
+    q, k, gain = torch.ones(2, 4, 64, dtype=torch.bfloat16), torch.ones(2, 2, 64, dtype=torch.bfloat16), torch.ones(64).bfloat16()
+    two, three = torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with forward_ad.dual_level():
+        dq, dk, dg = (forward_ad.make_dual(x, x.clone()) for x in (q, k, gain))
+        for f in (lambda: c.decode(dq, two), lambda: c.decode(q, two, out=dq), lambda: c.prefill(dq, two, three),
+                  lambda: c.prefill(q, two, three, out=dq), lambda: c.append(dq, k, k, two, two),
+                  lambda: c.append(q, dk, k, two, two), lambda: c.append(None, k, dk, two, two),
+                  lambda: c.append(q, k, k, two, two, q_norm=dg), lambda: c.append(q, k, k, two, two, k_norm=dg),
+                  lambda: c.append(q, k, k, two, two, q_out=dq),
+                  lambda: PagedCache(forward_ad.make_dual(c.k_pages, c.k_pages.clone()), c.v_pages, c.page_table),
+                  lambda: PagedCache(c.k_pages, forward_ad.make_dual(c.v_pages, c.v_pages.clone()), c.page_table)):
+            with pytest.raises(ValueError, match="tangent"):
+                f()
+        with pytest.raises(ValueError, match="one row per sequence"):   # others are checked as ever
+            c.decode(q[:1], two)
+
+
 # ---- the oracle
 def test_oracle_rotation_is_the_prompt_oracle_s():
     """One axis over the whole head: the same as the decoder oracle's rotation."""
