@@ -5,7 +5,8 @@ append rows to the pages and attend over them (include/gvc.h, "paged cache",
 says what each computes).  PyTorch provides memory and streams; every
 computation is a call into libgvc on the current stream of the cache's GPU,
 asynchronous and fit for capture into a graph.  There are no derivatives:
-tensors that require a gradient, and duals of forward mode, are refused.
+tensors that require a gradient are refused unless autograd is off
+(`torch.no_grad()`; pages and outputs always), and so are duals of forward mode.
 
     cache = PagedCache.empty(n_pages, page_size, n_kv_heads, head_dim, n_seqs, max_pages)
     q = cache.append(q, k, v, row_seq, row_slot, rope_pairs=(16, 24, 24), positions=thw)
@@ -204,7 +205,8 @@ class PagedCache:
     def _rows(self, t, name, heads):
         """(rows, row stride) of t [rows][heads][head_dim]."""
         shape = t.shape
-        if t.dtype != self._dtype or t.get_device() != self._index or len(shape) != 3 or t.requires_grad:
+        if t.dtype != self._dtype or t.get_device() != self._index or len(shape) != 3 or (
+                t.requires_grad and torch.is_grad_enabled()):
             raise ValueError(name + " must be [rows][heads][head_dim] of the pages' type and device, without gradient")
         n, h, dh = shape
         rs, hs, es = t.stride()
@@ -220,7 +222,7 @@ class PagedCache:
         if t is None:
             return None
         if (t.dtype != self._dtype or t.get_device() != self._index or t.shape != (self.head_dim,) or t.stride(0) != 1 or
-                t.requires_grad):
+                t.requires_grad and torch.is_grad_enabled()):
             raise ValueError(name + " must be a contiguous vector of head_dim of the pages' type and device, without "
                              "gradient")
         return t.data_ptr()
@@ -233,8 +235,8 @@ class PagedCache:
             # contiguous, whatever q's strides
             return heads, n, qs, torch.empty_like(q, memory_format=torch.contiguous_format), heads * self.head_dim
         m, os = self._rows(out, "the output", heads)
-        if m != n:
-            raise ValueError("the output must have q's rows")
+        if m != n or out.requires_grad:
+            raise ValueError("the output must have q's rows and not require a gradient")
         return heads, n, qs, out, os
 
     def _call(self, f, *args):

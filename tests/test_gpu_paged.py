@@ -915,3 +915,17 @@ def test_rounded_probabilities_do_not_carry_an_output_past_the_largest_value(t, 
     c.v_pages[pool.table[0, 0], 0, 7, 3] = float("-inf")   # an infinity in sight stays one
     out = c.prefill(q, pool.ints([n - 1] * rows), pool.ints([0, rows]), scale=scale)
     assert (out[:, :, 7] == float("-inf")).all() and (out[:, :, :7] == big).all() and (out[:, :, 8:] == big).all()
+
+
+def test_gains_that_are_parameters():
+    pool = Pool(68, "bf16", 2, 64, 16, [20, 20])
+    c, seq, slot = pool.cache, pool.ints([0, 1]), pool.ints([3, 4])
+    q, k, v = pool.rows(2, 4), pool.rows(2, 2), pool.rows(2, 2)
+    gain = torch.tensor(1 + 0.2 * pool.r.standard_normal(64)).to(torch.bfloat16).to(DEV)
+    want = c.append(q, k, v, seq, slot, q_norm=gain, k_norm=gain)
+    param = torch.nn.Parameter(gain.clone())
+    with torch.no_grad():
+        got = c.append(torch.nn.Parameter(q), k, v, seq, slot, q_norm=param, k_norm=param)
+    assert torch.equal(want, got) and not got.requires_grad
+    with pytest.raises(ValueError):
+        c.append(q, k, v, seq, slot, q_norm=param)

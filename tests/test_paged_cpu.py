@@ -217,6 +217,22 @@ def test_forward_mode_duals_are_refused():
             c.decode(q[:1], two)
 
 
+def test_parameters_are_taken_where_autograd_is_off():
+    """A model's norm gains are parameters; without a graph to record, nothing is lost."""
+    import torch
+    c = _host_cache()
+    gain = torch.nn.Parameter(torch.ones(64).bfloat16())
+    q, two = torch.nn.Parameter(torch.ones(2, 4, 64).bfloat16()), torch.zeros(2, dtype=torch.int32)
+    for off in (torch.no_grad, torch.inference_mode):
+        with off():
+            assert c._gain(gain, "q_norm") == gain.data_ptr() and c._rows(q, "q", 4) == (2, 256)
+            with pytest.raises(ValueError):   # never written to
+                c.decode(q, two, out=q)
+    for f in (lambda: c._gain(gain, "q_norm"), lambda: c._rows(q, "q", 4), lambda: c.decode(q, two)):
+        with pytest.raises(ValueError):
+            f()
+
+
 # ---- the oracle
 def test_oracle_rotation_is_the_prompt_oracle_s():
     """One axis over the whole head: the same as the decoder oracle's rotation."""
