@@ -25,6 +25,8 @@ _DTYPES = {torch.bfloat16: gvc.BF16, torch.float16: gvc.FP16}
 _shapes = {}
 _KEPT = 4096
 
+_INT = 2 ** 31   # numbers from here on would reach the C call cut to 32 bits
+
 
 def _kept(store, key, make):
     value = store.get(key)
@@ -107,8 +109,8 @@ class PagedCache:
         self._ints(row_seq, "row_seq", n)
         self._ints(row_slot, "row_slot", n)
         pairs = (self.head_dim // 2,) if rope_pairs is None else tuple(rope_pairs)
-        if len(pairs) > 3:
-            raise ValueError("rope_pairs has at most three axes")
+        if len(pairs) > 3 or pairs and not -_INT <= min(pairs) <= max(pairs) < _INT:
+            raise ValueError("rope_pairs has at most three axes, each a number of 32 bits")
         where = None
         if positions is not None:
             if (positions.dtype != torch.int32 or positions.get_device() != self._index or
@@ -187,6 +189,8 @@ class PagedCache:
         desc = self._descs.get(heads)
         if desc is None:
             dtype, n_pages, kv, page, dh, n_seqs, columns = self._shape
+            if max(n_pages, kv, page, dh, n_seqs, columns, heads) >= _INT:
+                raise ValueError("dimensions of pages and page table must fit 32 bits")
             desc = gvc.PagedDesc(_DTYPES[dtype], heads, kv, dh, page, n_pages, n_seqs, columns)
             self._descs[heads] = desc
         return desc
@@ -197,7 +201,7 @@ class PagedCache:
         key = (heads, prefill, n, window, sinks)
         size = self._sizes.get(key)
         if size is None:
-            if not (-2 ** 31 <= window < 2 ** 31 and -2 ** 31 <= sinks < 2 ** 31):   # the C call would see other numbers
+            if not (-_INT <= window < _INT and -_INT <= sinks < _INT):
                 raise ValueError("window and sinks must fit 32 bits")
             size = _kept(self._sizes, key, lambda: gvc.paged_workspace(desc, prefill, n, window, sinks))
         return torch.empty(size, dtype=torch.uint8, device=self.k_pages.device) if size else None
@@ -210,7 +214,7 @@ class PagedCache:
             raise ValueError(name + " must be [rows][heads][head_dim] of the pages' type and device, without gradient")
         n, h, dh = shape
         rs, hs, es = t.stride()
-        if h != heads or dh != self.head_dim or h < 1 or (n and (es != 1 or (h > 1 and hs != dh))):
+        if h != heads or dh != self.head_dim or h < 1 or n >= _INT or (n and (es != 1 or (h > 1 and hs != dh))):
             raise ValueError(name + " must be [rows][heads][head_dim] with dense heads")
         return n, rs if n > 1 else h * dh
 

@@ -233,6 +233,22 @@ def test_parameters_are_taken_where_autograd_is_off():
             f()
 
 
+def test_numbers_that_32_bits_would_cut_are_refused():
+    import torch
+    c = _host_cache()
+    q, k, two = torch.ones(2, 4, 64).bfloat16(), torch.ones(2, 2, 64).bfloat16(), torch.zeros(2, dtype=torch.int32)
+    for pairs in ((2 ** 32 + 8,), (8, 2 ** 32), (-2 ** 32 + 8, 8, 8), (2 ** 31,)):
+        with pytest.raises(ValueError, match="32 bits"):
+            c.append(q, k, k, two, two, rope_pairs=pairs)
+    with pytest.raises(ValueError):
+        c._rows(k[:1].expand(2 ** 32 + 1, 2, 64), "k", 2)
+    for at in range(1, 7):
+        c = _host_cache()
+        c._shape = tuple(2 ** 32 + x if i == at else x for i, x in enumerate(c._shape))
+        with pytest.raises(ValueError, match="32 bits"):
+            c._desc(4)
+
+
 # ---- the oracle
 def test_oracle_rotation_is_the_prompt_oracle_s():
     """One axis over the whole head: the same as the decoder oracle's rotation."""
