@@ -172,8 +172,9 @@ class PagedCache:
         """Raises GvcError where the page table, lengths or rows to be appended
         name a place that does not exist, or two rows the same one.  Copies
         them to the host: a debugging aid, not for the serving loop."""
-        host = [None if t is None else t.to("cpu", torch.int32).contiguous()
-                for t in (self.page_table, lengths, row_seq, row_slot)]
+        host = [t if t is None else t.to("cpu") for t in (self.page_table, lengths, row_seq, row_slot)]
+        # wider numbers than the calls take: to places as far outside
+        host = [t if t is None else t.to(torch.int64).clamp(-_INT, _INT - 1).to(torch.int32).contiguous() for t in host]
         if (row_seq is None) != (row_slot is None):
             raise ValueError("row_seq and row_slot come together")
         if lengths is not None and lengths.numel() != self.n_seqs:

@@ -249,6 +249,17 @@ def test_numbers_that_32_bits_would_cut_are_refused():
             c._desc(4)
 
 
+def test_check_of_64_bit_lists_cuts_no_number():
+    import torch
+    from paper_2608_10824_amd import gvc
+    c, far = _host_cache(), 2 ** 32
+    c.check(torch.tensor([48, 0]), torch.tensor([0, -1]), torch.tensor([47, far]))
+    for args in ((torch.tensor([far + 5, 0]),), (torch.tensor([-far, 0]),), (None, torch.tensor([far]), torch.tensor([3])),
+                 (None, torch.tensor([far - 1]), torch.tensor([3])), (None, torch.tensor([0]), torch.tensor([far + 3]))):
+        with pytest.raises(gvc.GvcError):
+            c.check(*args)
+
+
 # ---- the oracle
 def test_oracle_rotation_is_the_prompt_oracle_s():
     """One axis over the whole head: the same as the decoder oracle's rotation."""
