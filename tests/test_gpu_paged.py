@@ -929,3 +929,107 @@ def test_gains_that_are_parameters():
     assert torch.equal(want, got) and not got.requires_grad
     with pytest.raises(ValueError):
         c.append(q, k, v, seq, slot, q_norm=param)
+
+
+# ------------------------- calls of many sequences, many heads and large pools, by the path that they take
+def _fused(pool, window=0, sinks=0):
+    """(tiles of slots that a row sees at most, chunk length, whether units join themselves) as in k_paged_decode.hip."""
+    slots = pool.table.shape[1] * pool.page
+    most = min(-(-window // 32) + 1 + -(-sinks // 32) if window else 2 ** 30, -(-slots // 32))
+    least = -(-most // 8)
+    return most, least, least <= 8 or (least <= 32 and pool.kv * 8 >= 256)
+
+
+@pytest.mark.parametrize("t,dh,heads,kv", [("bf16", 64, 32, 32), ("fp16", 64, 64, 32), ("bf16", 128, 34, 34)])
+def test_units_of_many_heads_join_long_chunks_themselves(t, dh, heads, kv):
+    """2100 to 8192 slots of at least 32 key-value heads: eight long chunks and no second launch."""
+    lengths = [2700, 300, 0, 2100]
+    pool = Pool(71, t, kv, dh, 16, lengths, extra_columns=300)
+    most, least, fused = _fused(pool)
+    assert 64 < most <= 256 and least > 8 and fused
+    q = pool.rows(4, heads, 2.0)
+    for _ in range(2):   # the second in memory that the first has left
+        pool.expect(pool.cache.decode(q, pool.ints(lengths)), q, range(4), [n - 1 for n in lengths])
+    assert _fused(pool, 2200, 40)[1:] == (9, True)
+    pool.expect(pool.cache.decode(q, pool.ints(lengths), window=2200, sinks=40), q, range(4), [n - 1 for n in lengths], 2200, 40)
+    if 4 * kv <= 128:
+        rows = [range(2690, 2700), [299, 0], [], [2099]]
+        assert sum(len(x) for x in rows) * heads // kv <= 4 * 16
+        _ragged(pool, heads, rows)
+
+
+@pytest.mark.parametrize("seqs,kv,heads,columns", [(65, 2, 40, 0), (130, 2, 40, 0), (70, 1, 12, 200)])
+def test_tiles_of_many_sequences(seqs, kv, heads, columns):
+    """More sequences than a wave has lanes, some without rows, rows of no sequence before and behind."""
+    r = np.random.default_rng(72)
+    lengths = [int(n) for n in r.integers(0, 90, seqs)]
+    lengths[0], lengths[seqs - 1] = 90, 33
+    pool = Pool(72, "bf16", kv, 64, 16, lengths, extra_columns=columns)
+    lasts, seq, begin = [5] * 3, [-1] * 3, [3]
+    for s, n in enumerate(lengths):
+        new = 0 if s % 7 == 3 else min(n, int(r.integers(0, 60)))
+        lasts += range(n - new, n)
+        seq += [s] * new
+        begin.append(len(lasts))
+    lasts, seq = lasts + [4] * 5, seq + [-1] * 5
+    n = len(lasts)
+    _tiled(pool, n, heads)
+    q = pool.rows(n, heads, 2.0)
+    held = torch.full((n, heads, 64), 5.0, dtype=torch.bfloat16, device=DEV)
+    out = pool.cache.prefill(q, pool.ints(lasts), pool.ints(begin), out=held)
+    assert (held[:3] == 5).all() and (held[n - 5:] == 5).all()
+    pick = sorted({x for s in range(seqs) for x in (begin[s], begin[s + 1] - 1) if begin[s + 1] > begin[s]})
+    assert seq[pick[-1]] > 64 or seqs == 65
+    pool.expect(out[pick], q[pick], [seq[i] for i in pick], [lasts[i] for i in pick])
+
+
+@pytest.mark.parametrize("seqs,kv,columns", [(70, 2, 1000), (40, 4, 1700)])
+def test_tiles_of_one_row_to_a_sequence(seqs, kv, columns):
+    """One row of each of many sequences over a large table: 128-row tiles, whole and split over the slots."""
+    r = np.random.default_rng(73)
+    lengths = [int(n) for n in np.exp(r.uniform(0, 7, seqs))]
+    lengths[-1] = 1900
+    pool = Pool(73, "fp16", kv, 64, 16, lengths, extra_columns=columns)
+    heads = 2 * kv
+    assert seqs * heads * pool.table.shape[1] * 16 > 1 << 22 and seqs * kv > 128
+    _ragged(pool, heads, [[n - 1] for n in lengths])
+
+
+@pytest.mark.parametrize("length,fused", [(1500, True), (3000, False)])
+def test_few_rows_of_many_sequences(length, fused):
+    """Lists of few rows in 70 sequences, joined by their units and by a second launch, which looks a row's sequence up."""
+    r = np.random.default_rng(74)
+    lengths = [int(n) for n in r.integers(1, 100, 70)]
+    lengths[3], lengths[66] = length, length - 400
+    pool = Pool(74, "bf16", 1, 64, 16, lengths)
+    assert _fused(pool)[2] == fused
+    rows = [[n - 1] if s % 3 else [] for s, n in enumerate(lengths)]
+    rows[3], rows[66], rows[69] = [length - 1, 7], [length - 401, length - 402, 900], [0]
+    assert sum(len(x) for x in rows) * 8 <= 70 * 16
+    _ragged(pool, 8, rows)
+
+
+def test_tiles_over_four_gib():
+    """Pages whose byte offsets pass 32 bits, and a list long enough for 128-row tiles: the same bits as from a small pool."""
+    from paper_2608_10824_amd.paged import PagedCache
+    kv, dh, page, n_pages = 8, 128, 128, 17500   # 4.3 GiB each of keys and values
+    c = PagedCache.empty(n_pages, page, kv, dh, 2, 4, device=DEV)
+    pages = np.array([[n_pages - 1, 3, n_pages - 2, 8200], [1, n_pages - 3, 2, 0]], dtype=np.int32)
+    c.page_table.copy_(torch.tensor(pages))
+    g = torch.Generator(device=DEV).manual_seed(75)
+    for i in pages.flatten().tolist():
+        c.k_pages[i] = torch.randn(kv, page, dh, generator=g, device=DEV)
+        c.v_pages[i] = torch.randn(kv, dh, page, generator=g, device=DEV)
+    pool = Pool.__new__(Pool)
+    pool.t, pool.kv, pool.dh, pool.page, pool.table = "bf16", kv, dh, page, np.arange(8).reshape(2, 4)
+    at = torch.tensor(pages.flatten().astype(np.int64), device=DEV)
+    pool.cache = PagedCache(c.k_pages[at].clone(), c.v_pages[at].clone(), torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4))
+    lasts = list(range(512)) + list(range(400, 500))
+    n = len(lasts)
+    q = torch.randn(n, 16, dh, generator=g, device=DEV).to(torch.bfloat16)
+    _tiled(pool, n, 16)
+    args = (q, torch.tensor(lasts, dtype=torch.int32, device=DEV), torch.tensor([0, 512, n], dtype=torch.int32, device=DEV))
+    out = c.prefill(*args)
+    assert torch.equal(out, pool.cache.prefill(*args))
+    pick = [0, 130, 511, 512, n - 1]
+    pool.expect(out[pick], q[pick], [0, 0, 0, 1, 1], [lasts[i] for i in pick])
