@@ -369,7 +369,9 @@ int32_t gvc_destroy(gvc_ctx* ctx);
  * Rows: q, k, v and outputs are dev [rows][heads][head_dim] whose rows lie
  * `stride` elements apart (heads dense), so a fused projection's rows can be
  * given as they are; these pointers must be 16-byte aligned and the strides
- * multiples of 8.  Scores, softmax statistics and norms are fp32.  Calls are
+ * multiples of 8.  Scores, softmax statistics, sums and norms are fp32; a
+ * probability is rounded to the 16-bit type before it is multiplied with V.  An
+ * output is finite where the scores and the values that the row sees are.  Calls are
  * asynchronous on `stream` (NULL = the null stream) of the current GPU, may
  * be captured into a graph, and run on several streams at once if their
  * workspaces, outputs and written slots are apart.  out may be q itself (address

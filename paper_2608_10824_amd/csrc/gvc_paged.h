@@ -100,8 +100,8 @@ constexpr float kPagedLarge = 0x1p115f;
 // probability before the second product (whose operands are of one type: the matrix
 // cores would need two products for more bits.  Half a step, at most 2^-8 of it in bf16
 // and 2^-11 in fp16, averages out over the slots; the sum takes it unrounded) and an
-// output.  (Largest difference from 64 bits over the standard cases, bf16: 0.0018 to
-// 0.0022; with unrounded probabilities 0.0016 to 0.0017, the output's own rounding.)
+// output.  (Relative difference of bf16 outputs from 64 bits: 0.0018 to 0.0023; with
+// unrounded probabilities 0.0016 to 0.0017, the output's own rounding.)
 struct Bf16 {
   typedef pbf16x8 x8;
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));

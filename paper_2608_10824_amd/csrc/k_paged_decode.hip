@@ -18,10 +18,14 @@
 // result does not depend on which one that is; where there may be more than
 // kFuseChunks of them, by a second launch with a workgroup for each row.
 //
-// Measured (bf16, 128 to a head): one sequence of 282 slots, 32 heads, 7.1 us (a
+// Measured (bf16, 128 to a head): one sequence of 282 slots, 32 heads, 7.2 us (a
 // chain of launch, table, keys, values: 4.8 us for one slot); of 131072, 32 heads on
-// 8, 103.5 us, 5.2 TB/s; 16 sequences of 500 to 900 slots, 32 heads, 32.5 us, 4.5
-// TB/s; 64 of 5 to 16384 slots, 64 heads on 8, fp16, 123 us, 4.5 TB/s.
+// 8, 102.6 us, 5.2 TB/s; 16 sequences of 500 to 900 slots, 32 heads, 32.5 to 33.8 us, 4.3 to
+// 4.5 TB/s; 64 of 5 to 16384 slots, 64 heads on 8, fp16, 120 to 123 us, 4.5 TB/s.
+//
+// How a call is cut follows the table's width, which alone is known before the launch
+// (these figures: tables as wide as the longest sequence needs).  In a table of 8192
+// slots the 282 take 7.6 us, of 131072, with a second launch, 9.1 us.
 //
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMA.  A lane's scores in S^T are
 // of one query; the keys of a tile are ordered such that they are also the
@@ -138,8 +142,9 @@ __device__ __forceinline__ int long_chunk(const PagedAttnArgs& a, int G, int lea
 // Units are numbered through the sequences in order, chunk by chunk; a
 // sequence's row tiles all have the chunks that its last row would have.  Every
 // wave finds its unit by itself.
-// (4096 sequences of 100 slots, 32 heads on 8: 1305 us when all lengths were gone
-// through though none could be split, 401 without.)
+// (4096 sequences of 100 slots, 32 heads on 8: 368 to 401 us where the table holds less
+// than 512 slots each, so that none can be split; 985 to 1016 where it holds more and
+// all lengths are gone through.)
 template <bool ROWS>
 __device__ __forceinline__ Unit find_unit(const PagedAttnArgs& a, int G, int number, bool split, int least, int lane) {
   const int S = a.pool.n_seqs;
@@ -601,7 +606,9 @@ __global__ __launch_bounds__(NT) void k_paged_join(const PagedAttnArgs a, const 
 }
 
 // Lists of rows come here rather than to the 128-row tiles of the prefill
-// kernel where there is little to do in all (276 rows over 276 slots, 32 heads: 13.1 us
+// kernel where there is little to do in all, for all that a table of this width lets
+// them see (148 rows over 276 slots, 32 heads: 9.6 us, and 20 in the tiles, where they go
+// once the table holds 886 slots; 276 rows over 276 slots, 32 heads: 13.1 us
 // against 17.8; 300 over 300, 32 heads on 8: 13.8 against 17.1; 8 over 16000: 23.7
 // against 28.7; on the other side of the bound 128 over 2000: 28.9 against 25.6, 16
 // lists of 148 over 276, 32 heads: 77 against 37), or few sequences have one

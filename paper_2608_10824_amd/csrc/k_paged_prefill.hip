@@ -20,8 +20,8 @@
 // waits for all LDS reads where it needs one (5% slower), and a page's address
 // stays in scalar registers.
 //
-// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 527 us, 1044 TFLOP/s of
-// the products that rows see, 86% of a large matrix product's rate (matrix cores busy 52%,
+// Measured: 8192 causal rows, 32 heads of 128 on 8, bf16, 524 to 568 us by the box, 968 to 1048
+// TFLOP/s of the products that rows see, 80 to 86% of a large matrix product's rate (matrix cores busy 52%,
 // vector units 46% of the time: the softmax costs as much as the products, and
 // the two take turns); heads of 64 307 us, 896 TFLOP/s; 4 prompts of 1000 rows 58 us.
 #include "gvc_paged_rows.h"
