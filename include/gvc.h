@@ -415,7 +415,7 @@ typedef struct gvc_paged_rope {
  * slot (gvc_paged_check finds that), else either may be left there, element by
  * element.  q and q_out may both be NULL (keys and values only).  q_out may be
  * q itself (address and stride), else must not overlap the inputs.  n_rows *
- * max(n_heads + 2 n_kv_heads, 5) < 2^28.  Errors: GVC_EINVAL, GVC_EDEVICE. */
+ * (n_heads + 2 n_kv_heads) < 2^28 and n_rows * (8 + n_kv_heads) < 2^29 - 2^16.  Errors: GVC_EINVAL, GVC_EDEVICE. */
 int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
                          const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,

@@ -46,11 +46,11 @@ int32_t device(hipError_t e) noexcept {
 constexpr int64_t kMaxSlots = 1 << 30;
 // A launch has less than 2^32 threads.  Attention takes two to a row and head and
 // 256 to a sequence and key-value head, or at most 2^30 (short lists, and one row to
-// each of 4096 sequences).  Append takes 64 to a row and another 2^18 at most (a wave of
-// queries and keys, more only for fewer than 4096 rows) and 8 to a row and key-value
-// head (values): with heads counted as five at least, under 0.91 x 2^32.
+// each of 4096 sequences).  Append takes 64 to a row (a wave of queries and keys, more
+// only for fewer than 4096 rows) and 8 to a row and key-value head (values), and less than
+// 2^19 besides; with fewer than five heads in all that is more than the first bound allows.
 constexpr int64_t kMaxHeadRows = 1 << 28;
-constexpr int kAppendLeastHeads = 5;
+constexpr int64_t kMaxAppendThreads = ((int64_t)1 << 32) - (1 << 19);
 
 // nullptr, or what is wrong with d
 const char* bad_desc(const gvc_paged_desc* d) noexcept {
@@ -175,8 +175,9 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   // (a base below a float's range would turn by more than a double can reduce)
   if (!(rope->theta >= FLT_TRUE_MIN && rope->theta <= FLT_MAX)) return fail("theta must be positive and within a float's range");
   if (!(rope->rms_eps >= 0.f)) return fail("rms_eps must be >= 0");
-  if (n_rows < 0 || (int64_t)n_rows * std::max(d.n_heads + 2 * d.n_kv_heads, kAppendLeastHeads) >= kMaxHeadRows)
-    return fail("n_rows must be >= 0, and n_rows * max(n_heads + 2 n_kv_heads, 5) below 2^28");
+  if (n_rows < 0 || (int64_t)n_rows * (d.n_heads + 2 * d.n_kv_heads) >= kMaxHeadRows ||
+      (int64_t)n_rows * (64 + 8 * d.n_kv_heads) >= kMaxAppendThreads)
+    return fail("n_rows must be >= 0, n_rows * (n_heads + 2 n_kv_heads) below 2^28 and n_rows * (8 + n_kv_heads) below 2^29 - 2^16");
   if ((q == nullptr) != (q_out == nullptr) && n_rows) return fail("q and q_out come together");
   if (n_rows == 0) return GVC_OK;
   if (!row_seq || !row_slot || !k_pages || !v_pages || !page_table) return fail("null argument");

@@ -92,10 +92,10 @@ def test_bad_append_refused(kw):
     _refused(_append, _desc(), _rope(), **kw)
 
 
-@pytest.mark.parametrize("heads,kv,n", [(1, 1, 1 << 26), (1, 1, 53687092), (2, 1, (1 << 26) - 1), (2, 1, 53687092)])
+@pytest.mark.parametrize("heads,kv,n", [(1, 1, 1 << 26), (1, 1, 59645042), (2, 1, (1 << 26) - 1), (2, 1, 59645042)])
 def test_more_rows_than_a_launch_has_threads_refused(heads, kv, n):
     """n (heads + 2 kv) is below 2^28, but a row takes 64 threads and its values 8: 2^32 are the most."""
-    assert n * (heads + 2 * kv) < 1 << 28
+    assert n * (heads + 2 * kv) < 1 << 28 and n * (64 + 8 * kv) >= 2 ** 32 - 2 ** 19
     _refused(_append, _desc(n_heads=heads, n_kv_heads=kv), _rope(), n=n, qs=128)
 
 
