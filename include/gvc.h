@@ -1,6 +1,6 @@
 /*
  * gvc.h - C ABI of the Gated VLA-Cache control-step library for MI355X (gfx950).
- * The control step comes first; the paged cache's operators are at the end.
+ * The control step comes first; the operators of the paged caches (16 bits, then 8) are at the end.
  *
  * One control step of a Llama-2-shaped vision-language-action decoder in which
  * visually static image-patch tokens reuse the K/V they had at the previous
@@ -457,6 +457,63 @@ int32_t gvc_paged_prefill(const gvc_paged_desc* desc, float scale, int32_t windo
  * same place of the pool.  GVC_OK, or GVC_EINVAL with the first fault in gvc_last_error. */
 int32_t gvc_paged_check(const gvc_paged_desc* desc, const int32_t* page_table, const int32_t* lengths,
                         const int32_t* row_seq, const int32_t* row_slot, int32_t n_rows);
+
+/* --------------------------------------------------- quantised paged cache
+ * The paged cache with keys and values of 8 bits: about half the memory, and half
+ * of what a decode reads.  A head of a slot (head_dim values of K, or of V) is
+ * e4m3 codes (1 sign, 4 exponent bits of bias 7, 3 fraction bits; no infinities)
+ * and one scale code (e8m0), and stands for code * 2^(scale - 127) rounded to
+ * desc.dtype (in bf16 exact down to 2^-133); scale 255 is NaN.
+ *   k_pages: dev [n_pages][n_kv_heads][page_size][head_dim] codes
+ *   v_pages: dev [n_pages][n_kv_heads][head_dim][page_size] codes (dim-major)
+ *   k_scales, v_scales: dev [n_pages][n_kv_heads][page_size] scale codes
+ * All four 16-byte aligned.  Everything else is as for the paged cache above, the
+ * page table, rows, strides, what a row sees, streams and captures among it;
+ * gvc_paged_check checks these tables and lists as well.  q, outputs and norm gains
+ * have desc.dtype. */
+
+/* Rows into the pages, quantised as they are written: k after norm and rotation
+ * (of rope, as in gvc_paged_append; in fp32, with no rounding to 16 bits between),
+ * v as it is.  The scale of a head x is 2^e with the least e >= -126 for which
+ * max |x| <= 448 * 2^e, and its codes are x / 2^e rounded to nearest even.  Finite
+ * values past the largest code that the 16-bit type holds (61440 in fp16, 1.875 *
+ * 2^127 in bf16) become that one; NaN and infinities become NaN codes and do not count for
+ * the scale.  So rows that were read from a cache keep their values when they are
+ * appended without norm and rotation.  q_out gets q with norm and rotation in 16 bits.
+ * Rows, limits and errors as in gvc_paged_append. */
+int32_t gvc_quant_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
+                         const int32_t* row_slot, int32_t n_rows, void* k_pages, void* k_scales, void* v_pages,
+                         void* v_scales, const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream);
+
+/* Device bytes of workspace of gvc_quant_decode and gvc_quant_prefill, as gvc_paged_workspace. */
+int32_t gvc_quant_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
+                            int32_t n_sinks, size_t* bytes);
+
+/* gvc_paged_decode over a quantised cache. */
+int32_t gvc_quant_decode(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                         int64_t q_stride, const int32_t* lengths, const void* k_pages, const void* k_scales,
+                         const void* v_pages, const void* v_scales, const int32_t* page_table, void* out,
+                         int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* gvc_paged_prefill over a quantised cache. */
+int32_t gvc_quant_prefill(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                          int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows,
+                          const void* k_pages, const void* k_scales, const void* v_pages, const void* v_scales,
+                          const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Reads rows back in 16 bits: k_out, v_out dev [n_rows][n_kv_heads][head_dim]
+ * (rows k_stride and v_stride elements apart, as for q above; desc.n_heads does not
+ * matter) get what slot row_slot[r] of sequence row_seq[r] stands for, zeros for a row
+ * whose sequence, slot or page does not exist.  A finite value past the largest of fp16
+ * becomes an infinity.  Rows may name a slot several times.  Either output may be NULL;
+ * they must not overlap each other or the inputs.  n_rows * n_kv_heads < 2^28.
+ * Errors: GVC_EINVAL, GVC_EDEVICE. */
+int32_t gvc_quant_read(const gvc_paged_desc* desc, const int32_t* row_seq, const int32_t* row_slot, int32_t n_rows,
+                       const void* k_pages, const void* k_scales, const void* v_pages, const void* v_scales,
+                       const int32_t* page_table, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                       void* stream);
 
 /* Thread-local text of the last error ("" if none). */
 const char* gvc_last_error(void);

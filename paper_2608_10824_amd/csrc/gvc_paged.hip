@@ -1,6 +1,6 @@
-// Host side of the paged cache's operators: argument checks and launches of
-// the C ABI's gvc_paged_* calls.
-#include "gvc_paged.h"
+// Host side of the paged caches' operators: argument checks and launches of
+// the C ABI's gvc_paged_* and gvc_quant_* calls.
+#include "gvc_quant.h"
 
 #include <algorithm>
 #include <atomic>
@@ -69,10 +69,19 @@ const char* bad_desc(const gvc_paged_desc* d) noexcept {
   return nullptr;
 }
 
-PagedPool pool_of(const gvc_paged_desc& d, const void* k, const void* v, const int32_t* table) noexcept {
+// A call's pages: of 16 bits, or of codes with their scales.
+struct Pages {
+  const void *k, *v;
+  bool quant;
+  const void *k_scale, *v_scale;
+};
+
+PagedPool pool_of(const gvc_paged_desc& d, const Pages& pages, const int32_t* table) noexcept {
   PagedPool p{};
-  p.k = static_cast<uint16_t*>(const_cast<void*>(k));
-  p.v = static_cast<uint16_t*>(const_cast<void*>(v));
+  if (!pages.quant) {
+    p.k = static_cast<uint16_t*>(const_cast<void*>(pages.k));
+    p.v = static_cast<uint16_t*>(const_cast<void*>(pages.v));
+  }
   p.table = table;
   p.n_seqs = d.n_seqs;
   p.max_pages = d.max_pages;
@@ -84,7 +93,18 @@ PagedPool pool_of(const gvc_paged_desc& d, const void* k, const void* v, const i
   return p;
 }
 
+QuantPages quant_pages(const Pages& p) noexcept {
+  auto bytes = [](const void* x) { return static_cast<uint8_t*>(const_cast<void*>(x)); };
+  return {bytes(p.k), bytes(p.v), bytes(p.k_scale), bytes(p.v_scale)};
+}
+
 bool aligned(const void* p) noexcept { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+const char* bad_pages(const Pages& p, const int32_t* page_table) noexcept {
+  if (!p.k || !p.v || !page_table || (p.quant && (!p.k_scale || !p.v_scale))) return "null argument";
+  return aligned(p.k) && aligned(p.v) && aligned(p.k_scale) && aligned(p.v_scale) ? nullptr
+                                                                                  : "pages must be 16-byte aligned";
+}
 
 // rows of `heads` heads, `stride` elements apart
 const char* bad_rows(const void* p, int64_t stride, int heads, int dh, int n_rows) noexcept {
@@ -120,21 +140,21 @@ PagedSplit plan(const PagedPool& p, int n_rows, bool lists, const Reach& r, bool
 }
 
 int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
-               int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows, const void* k_pages,
-               const void* v_pages, const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
-               size_t workspace_bytes, void* stream) noexcept {
+               int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows, const Pages& pages,
+               const int32_t* page_table, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+               void* stream) noexcept {
   const gvc_paged_desc& d = *desc;
   const float scale_log2e = scale * 1.44269504088896340736f;
   if (!(scale > 0.f) || !std::isfinite(scale_log2e)) return fail("scale must be positive and finite (in powers of two too)");
   if (const char* w = bad_reach(window, n_sinks)) return fail(w);
   if (n_rows == 0) return GVC_OK;
-  if (!row_last || !k_pages || !v_pages || !page_table) return fail("null argument");
-  if (!aligned(k_pages) || !aligned(v_pages)) return fail("pages must be 16-byte aligned");
+  if (!row_last) return fail("null argument");
+  if (const char* w = bad_pages(pages, page_table)) return fail(w);
   if (const char* w = bad_rows(q, q_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
   if (const char* w = bad_rows(out, out_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
   const Reach seen = reach(d, window, n_sinks);
   PagedAttnArgs a{};
-  a.pool = pool_of(d, k_pages, v_pages, page_table);
+  a.pool = pool_of(d, pages, page_table);
   a.q = static_cast<const uint16_t*>(q);
   a.out = static_cast<uint16_t*>(out);
   a.q_stride = q_stride;
@@ -146,23 +166,20 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.n_sinks = seen.sinks;
   a.tag = paged_tag();
   a.scale_log2e = scale_log2e;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (pages.quant) return device(launch_quant_attend(a, quant_pages(pages), d.dtype, s));
   bool tiled;
   const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, tiled);
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))
     return set_error(GVC_ENOMEM, "the workspace is too small (or not 16-byte aligned)");
-  const hipStream_t s = static_cast<hipStream_t>(stream);
   return device(tiled ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
                       : launch_paged_decode(a, sp, d.dtype, workspace, s));
 }
 
-}  // namespace
-
-extern "C" {
-
-int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
-                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
-                         const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,
-                         const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream) {
+int32_t append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride, const void* k,
+               int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq, const int32_t* row_slot,
+               int32_t n_rows, const Pages& pages, const int32_t* page_table, void* q_out, int64_t q_out_stride,
+               void* stream) noexcept {
   if (const char* w = bad_desc(desc)) return fail(w);
   if (!rope) return fail("null rope");
   const gvc_paged_desc& d = *desc;
@@ -180,8 +197,8 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
     return fail("n_rows must be >= 0, n_rows * (n_heads + 2 n_kv_heads) below 2^28 and n_rows * (8 + n_kv_heads) below 2^29 - 2^16");
   if ((q == nullptr) != (q_out == nullptr) && n_rows) return fail("q and q_out come together");
   if (n_rows == 0) return GVC_OK;
-  if (!row_seq || !row_slot || !k_pages || !v_pages || !page_table) return fail("null argument");
-  if (!aligned(k_pages) || !aligned(v_pages)) return fail("pages must be 16-byte aligned");
+  if (!row_seq || !row_slot) return fail("null argument");
+  if (const char* w = bad_pages(pages, page_table)) return fail(w);
   if (q) {
     if (const char* w = bad_rows(q, q_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
     if (const char* w = bad_rows(q_out, q_out_stride, d.n_heads, d.head_dim, n_rows)) return fail(w);
@@ -191,7 +208,7 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   if (!aligned(rope->q_norm) || !aligned(rope->k_norm)) return fail("norm gains must be 16-byte aligned");
   if (rope->positions && rope->position_stride < n_rows) return fail("position_stride must be >= n_rows");
   PagedAppendArgs a{};
-  a.pool = pool_of(d, k_pages, v_pages, page_table);
+  a.pool = pool_of(d, pages, page_table);
   a.q = static_cast<const uint16_t*>(q);
   a.kin = static_cast<const uint16_t*>(k);
   a.vin = static_cast<const uint16_t*>(v);
@@ -215,39 +232,132 @@ int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope,
   const double step = n ? std::pow(rope->theta, -1.0 / (double)n) : 1.0;
   double turn = 0.15915494309189533577;
   for (int i = 0; i < n; ++i, turn *= step) a.turns[i] = turn;
-  return device(launch_paged_append(a, d.dtype, static_cast<hipStream_t>(stream)));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return device(pages.quant ? launch_quant_append(a, quant_pages(pages), d.dtype, s) : launch_paged_append(a, d.dtype, s));
 }
 
-int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
-                            int32_t n_sinks, size_t* bytes) {
+int32_t workspace_of(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window, int32_t n_sinks,
+                     size_t* bytes, bool quant) noexcept {
   if (const char* w = bad_desc(desc)) return fail(w);
   if (const char* w = bad_reach(window, n_sinks)) return fail(w);
   if (!bytes) return fail("null bytes");
   if (prefill && bad_row_count(*desc, n_rows)) return fail(bad_row_count(*desc, n_rows));
   bool tiled;
-  *bytes = plan(pool_of(*desc, nullptr, nullptr, nullptr), prefill ? n_rows : desc->n_seqs, prefill != 0,
-                reach(*desc, window, n_sinks), tiled).bytes;
+  *bytes = quant ? 0 : plan(pool_of(*desc, {}, nullptr), prefill ? n_rows : desc->n_seqs, prefill != 0,
+                            reach(*desc, window, n_sinks), tiled).bytes;
   return GVC_OK;
+}
+
+int32_t decode(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q, int64_t q_stride,
+               const int32_t* lengths, const Pages& pages, const int32_t* page_table, void* out, int64_t out_stride,
+               void* workspace, size_t workspace_bytes, void* stream) noexcept {
+  if (const char* w = bad_desc(desc)) return fail(w);
+  return attend(desc, scale, window, n_sinks, q, q_stride, lengths, nullptr, desc->n_seqs, pages, page_table, out,
+                out_stride, workspace, workspace_bytes, stream);
+}
+
+int32_t prefill(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows, const Pages& pages,
+                const int32_t* page_table, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                void* stream) noexcept {
+  if (const char* w = bad_desc(desc)) return fail(w);
+  if (const char* w = bad_row_count(*desc, n_rows)) return fail(w);
+  if (n_rows && !row_begin) return fail("null argument");
+  return attend(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, pages, page_table, out,
+                out_stride, workspace, workspace_bytes, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t gvc_paged_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
+                         const int32_t* row_slot, int32_t n_rows, void* k_pages, void* v_pages,
+                         const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream) {
+  return append(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows, {k_pages, v_pages},
+                page_table, q_out, q_out_stride, stream);
+}
+
+int32_t gvc_quant_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
+                         const int32_t* row_slot, int32_t n_rows, void* k_pages, void* k_scales, void* v_pages,
+                         void* v_scales, const int32_t* page_table, void* q_out, int64_t q_out_stride, void* stream) {
+  return append(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows,
+                {k_pages, v_pages, true, k_scales, v_scales}, page_table, q_out, q_out_stride, stream);
+}
+
+int32_t gvc_paged_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
+                            int32_t n_sinks, size_t* bytes) {
+  return workspace_of(desc, prefill, n_rows, window, n_sinks, bytes, false);
+}
+
+int32_t gvc_quant_workspace(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows, int32_t window,
+                            int32_t n_sinks, size_t* bytes) {
+  return workspace_of(desc, prefill, n_rows, window, n_sinks, bytes, true);
 }
 
 int32_t gvc_paged_decode(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
                          int64_t q_stride, const int32_t* lengths, const void* k_pages, const void* v_pages,
                          const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
                          size_t workspace_bytes, void* stream) {
-  if (const char* w = bad_desc(desc)) return fail(w);
-  return attend(desc, scale, window, n_sinks, q, q_stride, lengths, nullptr, desc->n_seqs, k_pages, v_pages, page_table,
-                out, out_stride, workspace, workspace_bytes, stream);
+  return decode(desc, scale, window, n_sinks, q, q_stride, lengths, {k_pages, v_pages}, page_table, out, out_stride,
+                workspace, workspace_bytes, stream);
+}
+
+int32_t gvc_quant_decode(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                         int64_t q_stride, const int32_t* lengths, const void* k_pages, const void* k_scales,
+                         const void* v_pages, const void* v_scales, const int32_t* page_table, void* out,
+                         int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  return decode(desc, scale, window, n_sinks, q, q_stride, lengths, {k_pages, v_pages, true, k_scales, v_scales},
+                page_table, out, out_stride, workspace, workspace_bytes, stream);
 }
 
 int32_t gvc_paged_prefill(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
                           int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows,
                           const void* k_pages, const void* v_pages, const int32_t* page_table, void* out,
                           int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  return prefill(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, {k_pages, v_pages}, page_table,
+                 out, out_stride, workspace, workspace_bytes, stream);
+}
+
+int32_t gvc_quant_prefill(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
+                          int64_t q_stride, const int32_t* row_last, const int32_t* row_begin, int32_t n_rows,
+                          const void* k_pages, const void* k_scales, const void* v_pages, const void* v_scales,
+                          const int32_t* page_table, void* out, int64_t out_stride, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  return prefill(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows,
+                 {k_pages, v_pages, true, k_scales, v_scales}, page_table, out, out_stride, workspace, workspace_bytes,
+                 stream);
+}
+
+int32_t gvc_quant_read(const gvc_paged_desc* desc, const int32_t* row_seq, const int32_t* row_slot, int32_t n_rows,
+                       const void* k_pages, const void* k_scales, const void* v_pages, const void* v_scales,
+                       const int32_t* page_table, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                       void* stream) {
   if (const char* w = bad_desc(desc)) return fail(w);
-  if (const char* w = bad_row_count(*desc, n_rows)) return fail(w);
-  if (n_rows && !row_begin) return fail("null argument");
-  return attend(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages, v_pages, page_table,
-                out, out_stride, workspace, workspace_bytes, stream);
+  const gvc_paged_desc& d = *desc;
+  if (n_rows < 0 || (int64_t)n_rows * d.n_kv_heads >= kMaxHeadRows)
+    return fail("n_rows must be >= 0, and n_rows * n_kv_heads below 2^28");
+  if (n_rows == 0 || (!k_out && !v_out)) return GVC_OK;
+  if (!row_seq || !row_slot) return fail("null argument");
+  const Pages pages{k_pages, v_pages, true, k_scales, v_scales};
+  if (const char* w = bad_pages(pages, page_table)) return fail(w);
+  if (k_out)
+    if (const char* w = bad_rows(k_out, k_stride, d.n_kv_heads, d.head_dim, n_rows)) return fail(w);
+  if (v_out)
+    if (const char* w = bad_rows(v_out, v_stride, d.n_kv_heads, d.head_dim, n_rows)) return fail(w);
+  QuantReadArgs a{};
+  a.pool = pool_of(d, pages, page_table);
+  a.pages = quant_pages(pages);
+  a.row_seq = row_seq;
+  a.row_slot = row_slot;
+  a.n_rows = n_rows;
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.v_out = static_cast<uint16_t*>(v_out);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  return device(launch_quant_read(a, d.dtype, static_cast<hipStream_t>(stream)));
 }
 
 int32_t gvc_paged_check(const gvc_paged_desc* desc, const int32_t* page_table, const int32_t* lengths,

@@ -26,7 +26,8 @@ EXPORTED = ("gvc_sizes", "gvc_init_cache", "gvc_select_static", "gvc_select_stat
             "gvc_decode_actions",
             "gvc_margin_gate", "gvc_invalidate", "gvc_read_state", "gvc_state_item_bytes", "gvc_profile_begin",
             "gvc_profile_end", "gvc_destroy", "gvc_last_error", "gvc_check_rows", "gvc_paged_append",
-            "gvc_paged_workspace", "gvc_paged_decode", "gvc_paged_prefill", "gvc_paged_check")
+            "gvc_paged_workspace", "gvc_paged_decode", "gvc_paged_prefill", "gvc_paged_check", "gvc_quant_append",
+            "gvc_quant_workspace", "gvc_quant_decode", "gvc_quant_prefill", "gvc_quant_read")
 
 
 class GvcError(RuntimeError):
@@ -116,6 +117,12 @@ def lib():
         L.gvc_paged_decode.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, sz, vp]
         L.gvc_paged_prefill.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, i64, vp, sz, vp]
         L.gvc_paged_check.argtypes = [pd, vp, vp, vp, vp, i32]
+        L.gvc_quant_append.argtypes = [pd, ctypes.POINTER(PagedRope), vp, i64, vp, i64, vp, i64, vp, vp, i32, vp, vp, vp,
+                                       vp, vp, vp, i64, vp]
+        L.gvc_quant_workspace.argtypes = L.gvc_paged_workspace.argtypes
+        L.gvc_quant_decode.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.gvc_quant_prefill.argtypes = [pd, f32, i32, i32, vp, i64, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.gvc_quant_read.argtypes = [pd, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]
         L.gvc_last_error.restype = ctypes.c_char_p
         for n in EXPORTED:
             if n not in ("gvc_state_item_bytes", "gvc_last_error"):
@@ -245,3 +252,34 @@ def paged_prefill(*args):
 def paged_check(desc: PagedDesc, page_table: int, lengths, row_seq, row_slot, n_rows: int):
     """Host-side check (all arguments host addresses, lengths and rows may be None); raises GvcError on a fault."""
     _check(lib().gvc_paged_check(desc, page_table, lengths, row_seq, row_slot, n_rows))
+
+
+# ---- the quantised paged cache (gvc_quant_*), with the arguments of the calls above
+def quant_append(*args):
+    """(desc, rope, q, q_stride, k, k_stride, v, v_stride, row_seq, row_slot, n_rows, k_pages, k_scales, v_pages,
+    v_scales, page_table, q_out, q_out_stride, stream)"""
+    _check((_lib or lib()).gvc_quant_append(*args))
+
+
+def quant_workspace(desc: PagedDesc, prefill: bool, n_rows: int, window: int = 0, n_sinks: int = 0) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().gvc_quant_workspace(desc, int(prefill), n_rows, window, n_sinks, ctypes.byref(n)))
+    return n.value
+
+
+def quant_decode(*args):
+    """(desc, scale, window, n_sinks, q, q_stride, lengths, k_pages, k_scales, v_pages, v_scales, page_table, out,
+    out_stride, workspace, workspace_bytes, stream)"""
+    _check((_lib or lib()).gvc_quant_decode(*args))
+
+
+def quant_prefill(*args):
+    """(desc, scale, window, n_sinks, q, q_stride, row_last, row_begin, n_rows, k_pages, k_scales, v_pages, v_scales,
+    page_table, out, out_stride, workspace, workspace_bytes, stream)"""
+    _check((_lib or lib()).gvc_quant_prefill(*args))
+
+
+def quant_read(*args):
+    """(desc, row_seq, row_slot, n_rows, k_pages, k_scales, v_pages, v_scales, page_table, k_out, k_stride, v_out,
+    v_stride, stream)"""
+    _check((_lib or lib()).gvc_quant_read(*args))

@@ -1,10 +1,12 @@
-"""The paged key-value cache over PyTorch tensors.
+"""The paged key-value caches over PyTorch tensors.
 
 A `PagedCache` holds the pages and the page table of one layer; its calls
 append rows to the pages and attend over them (include/gvc.h, "paged cache",
-says what each computes).  PyTorch provides memory and streams; every
-computation is a call into libgvc on the current stream of the cache's GPU,
-asynchronous and fit for capture into a graph.  There are no derivatives:
+says what each computes).  A `QuantPagedCache` has the same calls over pages of
+8 bits ("quantised paged cache"), and reads rows back in 16.  PyTorch provides
+memory and streams; every computation is a call into libgvc on the current
+stream of the cache's GPU, asynchronous and fit for capture into a graph.  There
+are no derivatives:
 tensors that require a gradient are refused unless autograd is off
 (`torch.no_grad()`; pages and outputs always), and so are duals of forward mode.
 
@@ -12,6 +14,10 @@ tensors that require a gradient are refused unless autograd is off
     q = cache.append(q, k, v, row_seq, row_slot, rope_pairs=(16, 24, 24), positions=thw)
     o = cache.prefill(q, row_slot, row_begin)            # the rows of a prompt
     o = cache.decode(q, lengths, window=4096, sinks=4)   # one new token per sequence
+
+    cache = QuantPagedCache.empty(n_pages, page_size, n_kv_heads, head_dim, n_seqs, max_pages)
+    q = cache.append(q, k, v, row_seq, row_slot)         # and prefill and decode, as above
+    k, v = cache.read(row_seq, row_slot)                 # rows back in 16 bits
 """
 import torch
 from torch.autograd import forward_ad
@@ -53,13 +59,16 @@ class PagedCache:
     page_table int32 [n_seqs][max_pages], all contiguous on one GPU.  The
     tensors stay the caller's: the table may be changed between calls."""
 
+    _append, _decode = staticmethod(gvc.paged_append), staticmethod(gvc.paged_decode)
+    _prefill, _workspace_size = staticmethod(gvc.paged_prefill), staticmethod(gvc.paged_workspace)
+
     def __init__(self, k_pages, v_pages, page_table):
         dtype = k_pages.dtype
         if dtype not in _DTYPES or v_pages.dtype != dtype:
             raise ValueError("pages must be bfloat16 or float16, both alike")
         if k_pages.dim() != 4:
             raise ValueError("k_pages must be [n_pages][n_kv_heads][page_size][head_dim]")
-        n_pages, kv, page, dh = shape = k_pages.shape
+        n_pages, kv, page, dh = k_pages.shape
         if v_pages.shape != (n_pages, kv, dh, page):
             raise ValueError("v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
         if page_table.dtype != torch.int32 or page_table.dim() != 2:
@@ -73,12 +82,16 @@ class PagedCache:
         index = k_pages.get_device()
         if index < 0 or v_pages.get_device() != index or page_table.get_device() != index:
             raise ValueError("pages and page table must be on one GPU")
+        self._hold(k_pages, v_pages, page_table, dtype, index, False)
+
+    def _hold(self, k_pages, v_pages, page_table, dtype, index, quant):
         self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
         self.n_seqs, columns = page_table.shape
-        self.n_kv_heads, self.head_dim = kv, dh
+        shape = k_pages.shape
+        self.n_kv_heads, self.head_dim = shape[1], shape[3]
         self._dtype, self._index = dtype, index
         self._shape = (dtype, *shape, self.n_seqs, columns)
-        self._descs, self._sizes = _kept(_shapes, self._shape, lambda: ({}, {}))
+        self._descs, self._sizes = _kept(_shapes, (quant, self._shape), lambda: ({}, {}))
 
     @property
     def device(self):
@@ -128,9 +141,8 @@ class PagedCache:
             if m != n:
                 raise ValueError("q and k must have the same rows")
             qp, op = q.data_ptr(), q_out.data_ptr()
-        self._call(gvc.paged_append, self._desc(heads), rope, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs,
-                   row_seq.data_ptr(), row_slot.data_ptr(), n, self.k_pages.data_ptr(), self.v_pages.data_ptr(),
-                   self.page_table.data_ptr(), op, os)
+        self._call(self._append, self._desc(heads), rope, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                   row_seq.data_ptr(), row_slot.data_ptr(), n, *self._pages(), op, os)
         return q_out
 
     def decode(self, q, lengths, *, scale=None, window=0, sinks=0, out=None):
@@ -145,9 +157,8 @@ class PagedCache:
         self._ints(lengths, "lengths", n)
         desc = self._desc(heads)
         work = self._workspace(desc, heads, False, n, window, sinks)
-        self._call(gvc.paged_decode, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks, q.data_ptr(),
-                   qs, lengths.data_ptr(), self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(),
-                   out.data_ptr(), os, *_address(work))
+        self._call(self._decode, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks, q.data_ptr(),
+                   qs, lengths.data_ptr(), *self._pages(), out.data_ptr(), os, *_address(work))
         return out
 
     def prefill(self, q, row_last, row_begin, *, scale=None, window=0, sinks=0, out=None):
@@ -163,9 +174,9 @@ class PagedCache:
         self._ints(row_begin, "row_begin", self.n_seqs + 1)
         desc = self._desc(heads)
         work = self._workspace(desc, heads, True, n, window, sinks)
-        self._call(gvc.paged_prefill, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks,
-                   q.data_ptr(), qs, row_last.data_ptr(), row_begin.data_ptr(), n, self.k_pages.data_ptr(),
-                   self.v_pages.data_ptr(), self.page_table.data_ptr(), out.data_ptr(), os, *_address(work))
+        self._call(self._prefill, desc, self.head_dim ** -0.5 if scale is None else scale, window, sinks,
+                   q.data_ptr(), qs, row_last.data_ptr(), row_begin.data_ptr(), n, *self._pages(), out.data_ptr(), os,
+                   *_address(work))
         return out
 
     def check(self, lengths=None, row_seq=None, row_slot=None):
@@ -185,6 +196,10 @@ class PagedCache:
                         0 if row_seq is None else row_seq.numel())
 
     # ---- argument checks and marshalling
+    def _pages(self):
+        """Addresses of the pages and the page table."""
+        return self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr()
+
     def _desc(self, heads):
         """The descriptor for this many query heads."""
         desc = self._descs.get(heads)
@@ -204,7 +219,7 @@ class PagedCache:
         if size is None:
             if not (-_INT <= window < _INT and -_INT <= sinks < _INT):
                 raise ValueError("window and sinks must fit 32 bits")
-            size = _kept(self._sizes, key, lambda: gvc.paged_workspace(desc, prefill, n, window, sinks))
+            size = _kept(self._sizes, key, lambda: self._workspace_size(desc, prefill, n, window, sinks))
         return torch.empty(size, dtype=torch.uint8, device=self.k_pages.device) if size else None
 
     def _rows(self, t, name, heads):
@@ -250,3 +265,86 @@ class PagedCache:
             with torch.cuda.device(self._index):
                 return f(*args, torch._C._cuda_getCurrentRawStream(self._index))
         return f(*args, torch._C._cuda_getCurrentRawStream(self._index))
+
+
+class QuantPagedCache(PagedCache):
+    """A paged cache of 8 bits: codes k_pages [n_pages][n_kv_heads][page_size][head_dim]
+    and v_pages [n_pages][n_kv_heads][head_dim][page_size] (float8_e4m3fn), a scale
+    for each head of a slot in k_scales and v_scales [n_pages][n_kv_heads][page_size]
+    (float8_e8m0fnu: powers of two), and page_table as in PagedCache.  A head of a slot
+    is its codes times its scale in `dtype` (bfloat16 or float16), which is also the
+    type of q, k, v and outputs; `append` quantises k and v as it writes them."""
+
+    _append, _decode = staticmethod(gvc.quant_append), staticmethod(gvc.quant_decode)
+    _prefill, _workspace_size = staticmethod(gvc.quant_prefill), staticmethod(gvc.quant_workspace)
+
+    def __init__(self, k_pages, k_scales, v_pages, v_scales, page_table, dtype=torch.bfloat16):
+        if dtype not in _DTYPES:
+            raise ValueError("dtype must be bfloat16 or float16")
+        if k_pages.dtype != torch.float8_e4m3fn or v_pages.dtype != torch.float8_e4m3fn:
+            raise ValueError("pages must be float8_e4m3fn")
+        if k_scales.dtype != torch.float8_e8m0fnu or v_scales.dtype != torch.float8_e8m0fnu:
+            raise ValueError("scales must be float8_e8m0fnu")
+        if k_pages.dim() != 4:
+            raise ValueError("k_pages must be [n_pages][n_kv_heads][page_size][head_dim]")
+        n_pages, kv, page, dh = k_pages.shape
+        if v_pages.shape != (n_pages, kv, dh, page):
+            raise ValueError("v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
+        if k_scales.shape != (n_pages, kv, page) or v_scales.shape != (n_pages, kv, page):
+            raise ValueError("scales must be [n_pages][n_kv_heads][page_size]")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [n_seqs][max_pages]")
+        index = k_pages.get_device()
+        for t in (k_pages, k_scales, v_pages, v_scales):
+            if t.requires_grad:
+                raise ValueError("pages must not require a gradient")
+            if not t.is_contiguous():
+                raise ValueError("pages, scales and page table must be contiguous")
+            if t.get_device() != index:
+                raise ValueError("pages, scales and page table must be on one GPU")
+        if not page_table.is_contiguous():
+            raise ValueError("pages, scales and page table must be contiguous")
+        if index < 0 or page_table.get_device() != index:
+            raise ValueError("pages, scales and page table must be on one GPU")
+        if forward_ad._current_level >= 0:
+            _no_tangents(k_pages, k_scales, v_pages, v_scales)
+        self.k_scales, self.v_scales = k_scales, v_scales
+        self._hold(k_pages, v_pages, page_table, dtype, index, True)
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, n_seqs, max_pages, dtype=torch.bfloat16, device="cuda"):
+        """A cache of its own memory, no page of it in the table yet (every entry -1)."""
+        def zeros(t, *shape):
+            return torch.zeros(n_pages, n_kv_heads, *shape, dtype=torch.uint8, device=device).view(t)
+        return cls(zeros(torch.float8_e4m3fn, page_size, head_dim), zeros(torch.float8_e8m0fnu, page_size),
+                   zeros(torch.float8_e4m3fn, head_dim, page_size), zeros(torch.float8_e8m0fnu, page_size),
+                   torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), dtype)
+
+    def read(self, row_seq, row_slot, *, k_out=None, v_out=None):
+        """(k, v) [rows][n_kv_heads][head_dim] of slots row_slot[r] of sequences
+        row_seq[r] (int32) in 16 bits, zeros for a row whose place does not exist."""
+        if forward_ad._current_level >= 0:
+            _no_tangents(k_out, v_out)
+        n, kv = row_seq.numel(), self.n_kv_heads
+        self._ints(row_seq, "row_seq", n)
+        self._ints(row_slot, "row_slot", n)
+        if n >= _INT:
+            raise ValueError("rows must fit 32 bits")
+        (k_out, ks), (v_out, vs) = self._read_out(k_out, "k_out", n), self._read_out(v_out, "v_out", n)
+        self._call(gvc.quant_read, self._desc(kv), row_seq.data_ptr(), row_slot.data_ptr(), n, *self._pages(),
+                   k_out.data_ptr(), ks, v_out.data_ptr(), vs)
+        return k_out, v_out
+
+    def _read_out(self, out, name, n):
+        """The given or a new output of n rows, and its row stride."""
+        kv = self.n_kv_heads
+        if out is None:
+            return torch.empty(n, kv, self.head_dim, dtype=self._dtype, device=self.k_pages.device), kv * self.head_dim
+        m, stride = self._rows(out, name, kv)
+        if m != n or out.requires_grad:
+            raise ValueError("%s must have a row for each of row_seq and not require a gradient" % name)
+        return out, stride
+
+    def _pages(self):
+        return (self.k_pages.data_ptr(), self.k_scales.data_ptr(), self.v_pages.data_ptr(), self.v_scales.data_ptr(),
+                self.page_table.data_ptr())
