@@ -134,8 +134,9 @@ Reach reach(const gvc_paged_desc& d, int32_t window, int32_t n_sinks) noexcept {
 }
 
 // The kernel that a call takes (tiled: the prefill kernel) and how it is cut.
-PagedSplit plan(const PagedPool& p, int n_rows, bool lists, const Reach& r, bool& tiled) noexcept {
+PagedSplit plan(const PagedPool& p, int n_rows, bool lists, const Reach& r, bool quant, bool& tiled) noexcept {
   tiled = lists && !paged_few_rows(p, n_rows, r.window, r.sinks);
+  if (quant) return tiled ? PagedSplit{} : quant_decode_split(p, n_rows, lists, r.window, r.sinks);
   return tiled ? paged_prefill_split(p, n_rows) : paged_decode_split(p, n_rows, lists, r.window, r.sinks);
 }
 
@@ -167,11 +168,13 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   a.tag = paged_tag();
   a.scale_log2e = scale_log2e;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (pages.quant) return device(launch_quant_attend(a, quant_pages(pages), d.dtype, s));
   bool tiled;
-  const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, tiled);
+  const PagedSplit sp = plan(a.pool, n_rows, row_begin != nullptr, seen, pages.quant, tiled);
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))
     return set_error(GVC_ENOMEM, "the workspace is too small (or not 16-byte aligned)");
+  if (pages.quant)
+    return device(tiled ? launch_quant_attend(a, quant_pages(pages), d.dtype, s)
+                        : launch_quant_decode(a, quant_pages(pages), sp, d.dtype, workspace, s));
   return device(tiled ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
                       : launch_paged_decode(a, sp, d.dtype, workspace, s));
 }
@@ -243,8 +246,8 @@ int32_t workspace_of(const gvc_paged_desc* desc, int32_t prefill, int32_t n_rows
   if (!bytes) return fail("null bytes");
   if (prefill && bad_row_count(*desc, n_rows)) return fail(bad_row_count(*desc, n_rows));
   bool tiled;
-  *bytes = quant ? 0 : plan(pool_of(*desc, {}, nullptr), prefill ? n_rows : desc->n_seqs, prefill != 0,
-                            reach(*desc, window, n_sinks), tiled).bytes;
+  *bytes = plan(pool_of(*desc, {}, nullptr), prefill ? n_rows : desc->n_seqs, prefill != 0, reach(*desc, window, n_sinks),
+                quant, tiled).bytes;
   return GVC_OK;
 }
 

@@ -11,6 +11,8 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 
 // The lowest n of eight bits, for any n.
 __device__ __forceinline__ uint32_t first8(int n) { return (1u << min(max(n, 0), 8)) - 1; }
+// The same of sixteen.
+__device__ __forceinline__ uint32_t first16(int n) { return (1u << min(max(n, 0), 16)) - 1; }
 // x if bit i is set, else -infinity: two instructions and no condition register.
 __device__ __forceinline__ float seen_score(uint32_t bits, int i, float x) {
   const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)bits, i, 1);

@@ -41,8 +41,12 @@ __global__ __launch_bounds__(64) void k_quant_append(const PagedAppendArgs a, co
       const int pos = a.positions ? a.positions[axis * a.position_stride + row] : slot;
       double t = (double)pos * a.turns[pair];
       t -= rint(t);
+      t *= 2;
       float sn, cs;
-      sincospif((float)(2 * t), &sn, &cs);
+      sincospif((float)t, &sn, &cs);
+      const float rest = (float)(t - (double)(float)t) * 3.14159274f, s0 = sn;   // what fp32 cut from the angle
+      sn = fmaf(cs, rest, sn);
+      cs = fmaf(-s0, rest, cs);
       x[i] = d < n ? x[i] * cs - lds[d + n] * sn : x[i] * cs + lds[d - n] * sn;
     }
   }

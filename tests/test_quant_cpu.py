@@ -118,6 +118,27 @@ def test_nothing_to_do():
     _read(_desc(), k=None, v=None)
 
 
+def test_short_workspace_refused():
+    from paper_2608_10824_amd import gvc
+    d = _desc(max_pages=1000)
+    need = gvc.quant_workspace(d, False, 2)
+    assert need > 0
+    _refused(_decode, d, code=gvc.GVC_ENOMEM)
+    _refused(_decode, d, work=P, size=need - 1, code=gvc.GVC_ENOMEM)
+    _refused(_decode, d, work=P + 8, size=need, code=gvc.GVC_ENOMEM)
+    _refused(_prefill, d, work=None, size=need, code=gvc.GVC_ENOMEM)
+    _refused(gvc.quant_workspace, d, True, 1 << 28)
+    _refused(gvc.quant_workspace, d, False, 1, -1, 0)
+
+
+def test_largest_tables():
+    """2^30 slots in a row of the table and 2^27 entries in all are the most."""
+    from paper_2608_10824_amd import gvc
+    assert gvc.quant_workspace(_desc(n_seqs=4096, max_pages=1 << 15), False, 4096) > 0
+    assert gvc.quant_workspace(_desc(n_seqs=1, max_pages=1 << 26), False, 1) > 0
+    _refused(gvc.quant_workspace, _desc(n_seqs=4096, max_pages=(1 << 15) + 1), False, 4096)
+
+
 # ---- the wrapper
 def _tensors():
     import torch
