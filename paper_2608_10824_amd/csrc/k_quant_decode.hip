@@ -72,7 +72,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
   bool any = false;
   // The wave's tiles go round the waves.  Page ids of 16 of them at a time, a quarter
   // of a tile (16 slots, always one page) to a lane.
-  int ids = -1, ids_base = 0, id[4];
+  int ids = -1, ids_base = 0, k_id = -1, v_id = -1;   // pages of the lane's keys and values
   auto load_ids = [&](int n) {   // of the wave's tiles n .. n + 15
     const int t = t0 + (n + (lane >> 2)) * NW;
     const int j = tile_slot(min(t, max(t_end - 1, 0))) + 16 * (lane & 3);
@@ -82,17 +82,16 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
   };
   auto page_ids = [&](int n) {
     if (n - ids_base >= 16) load_ids(n);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) id[i] = __builtin_amdgcn_readlane(ids, 4 * (n - ids_base) + i);
+    k_id = __shfl(ids, 4 * (n - ids_base) + (col >> 2));
+    v_id = __shfl(ids, 4 * (n - ids_base) + g);
   };
-  auto id_of = [&](int quarter) { return quarter < 2 ? quarter ? id[1] : id[0] : quarter == 2 ? id[2] : id[3]; };
-  auto head_at = [&](int quarter) { return (int64_t)max(id_of(quarter), 0) * p.Hk + kvh; };
+  auto head_of_page = [&](int id) { return (int64_t)max(id, 0) * p.Hk + kvh; };
   // Operands of tile t, if there is one more; else the start of the pool, once
   // for all lanes: a branch around the loads would cost the waits for them
   // their order.  Keys in rows 4 g' + i of operand e are slots 16 g' + 4 e + i.
   pu32x4 kf[4][NK], vf[NO], ks, vs;
   auto load_k = [&](int t, bool more) {
-    const int64_t head = head_at(col >> 2) << p.page_shift;
+    const int64_t head = head_of_page(k_id) << p.page_shift;
     const int j = (tile_slot(t) + 16 * (col >> 2)) & in_page;
     const uint8_t* kp = from.k + (more ? (head + j + (col & 3)) * DH + g * 16 : 0);
     ks = *(const pu32x4*)(from.k_scale + (more ? head + j : 0));
@@ -102,7 +101,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
       for (int kk = 0; kk < NK; ++kk) kf[e][kk] = *(const pu32x4*)(kp + e * 4 * DH + kk * 64);
   };
   auto load_v = [&](int t, bool more) {
-    const int64_t head = head_at(g);
+    const int64_t head = head_of_page(v_id);
     const int j = (tile_slot(t) + 16 * g) & in_page;
     const uint8_t* vp = from.v + (more ? ((head * DH + col) << p.page_shift) + j : 0);
     vs = *(const pu32x4*)(from.v_scale + (more ? (head << p.page_shift) + j : 0));
@@ -170,8 +169,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
   for (int t = t0, n = 0; t < t_end; ++n) {
     const int j0 = tile_slot(t), next = t + NW;
     const bool more = next < t_end;
-    const bool okv = id_of(g) >= 0;
-    const bool full = min(min(id[0], id[1]), min(id[2], id[3])) >= 0 && j0 + 63 <= hi_all && j0 > lo_all;
+    const bool okv = v_id >= 0;
+    const bool full = __all(okv) && j0 + 63 <= hi_all && j0 > lo_all;
     pf32x4 s[4];
     scores(s);
     if (more) page_ids(n + 1);
@@ -241,7 +240,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
 #pragma unroll
         for (int u = 0; u < 16; ++u) {
           const int j = j0 + 16 * g + u;
-          const bool in = (id_of(g) >= 0) & (j <= last) & ((j > lo) | (j < a.n_sinks));
+          const bool in = (v_id >= 0) & (j <= last) & ((j > lo) | (j < a.n_sinks));
           x[u] = in ? s[u >> 2][u & 3] : -INFINITY;
           seen |= (unsigned)in << u;
           top = fmaxf(top, x[u]);
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_quant_decode(const PagedAttnArgs
 #pragma unroll 1
           for (int o = 0; o < 4; ++o) {   // the slots of lane group o
             const unsigned bits = (unsigned)__shfl((int)seen, 16 * o + col);
-            const int64_t head = head_at(o);
+            const int64_t head = head_of_page(__builtin_amdgcn_readlane(ids, 4 * (n - ids_base) + o));
             const int off = (j0 + 16 * o) & in_page;
             const uint8_t* vp = from.v + ((head * DH + 4 * g) << p.page_shift) + off;
             const uint8_t* sp = from.v_scale + (head << p.page_shift) + off;
