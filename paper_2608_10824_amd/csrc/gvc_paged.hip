@@ -136,8 +136,9 @@ Reach reach(const gvc_paged_desc& d, int32_t window, int32_t n_sinks) noexcept {
 // The kernel that a call takes (tiled: the prefill kernel) and how it is cut.
 PagedSplit plan(const PagedPool& p, int n_rows, bool lists, const Reach& r, bool quant, bool& tiled) noexcept {
   tiled = lists && !paged_few_rows(p, n_rows, r.window, r.sinks);
-  if (quant) return tiled ? PagedSplit{} : quant_decode_split(p, n_rows, lists, r.window, r.sinks);
-  return tiled ? paged_prefill_split(p, n_rows) : paged_decode_split(p, n_rows, lists, r.window, r.sinks);
+  if (tiled) return paged_prefill_split(p, n_rows);
+  return quant ? quant_decode_split(p, n_rows, lists, r.window, r.sinks)
+               : paged_decode_split(p, n_rows, lists, r.window, r.sinks);
 }
 
 int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t n_sinks, const void* q,
@@ -173,7 +174,7 @@ int32_t attend(const gvc_paged_desc* desc, float scale, int32_t window, int32_t 
   if (sp.bytes && (workspace_bytes < sp.bytes || !workspace || !aligned(workspace)))
     return set_error(GVC_ENOMEM, "the workspace is too small (or not 16-byte aligned)");
   if (pages.quant)
-    return device(tiled ? launch_quant_attend(a, quant_pages(pages), d.dtype, s)
+    return device(tiled ? launch_quant_prefill(a, quant_pages(pages), sp, d.dtype, workspace, s)
                         : launch_quant_decode(a, quant_pages(pages), sp, d.dtype, workspace, s));
   return device(tiled ? launch_paged_prefill(a, sp, d.dtype, workspace, s)
                       : launch_paged_decode(a, sp, d.dtype, workspace, s));

@@ -27,7 +27,8 @@ hipError_t launch_quant_read(const QuantReadArgs& a, int dtype, hipStream_t s);
 PagedSplit quant_decode_split(const PagedPool& p, int n_rows, bool rows, int window, int n_sinks);
 hipError_t launch_quant_decode(const PagedAttnArgs& a, const QuantPages& from, const PagedSplit& sp, int dtype,
                                void* workspace, hipStream_t s);
-hipError_t launch_quant_attend(const PagedAttnArgs& a, const QuantPages& from, int dtype, hipStream_t s);
+hipError_t launch_quant_prefill(const PagedAttnArgs& a, const QuantPages& from, const PagedSplit& sp, int dtype,
+                                void* workspace, hipStream_t s);
 
 #ifdef __HIPCC__
 // ------------------------------------------------------------------ device

@@ -24,47 +24,15 @@
 // TFLOP/s of the products that rows see, 80 to 86% of a large matrix product's rate (matrix cores busy 52%,
 // vector units 46% of the time: the softmax costs as much as the products, and
 // the two take turns); heads of 64 307 us, 896 TFLOP/s; 4 prompts of 1000 rows 58 us.
-#include "gvc_paged_rows.h"
+#include "gvc_paged_tiles.h"
 #include "gvc_sync.h"
 
 #define LPA(p) ((void __attribute__((address_space(3)))*)(p))
 
 namespace gvc {
 
-constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves, kPreKeys = 64;
-constexpr int kPreUnits = 512;   // calls with fewer units split the slots, into about as many
-constexpr int kPreMinTiles = 4;  // tiles of a part, at least
-constexpr int kPreMaxParts = kPreUnits;
-
 // Kinds of instructions for sched_group_barrier.
 constexpr int kMfma = 0x8, kDsRead = 0x100;
-
-// The tile of virtual rows that a workgroup takes.
-struct RowTile {
-  int seq, first, begin, rows;   // sequence (-1: none), the tile's first virtual row, the sequence's first row, its virtual rows
-};
-
-// Tile `number` of the call, counted from the last sequence's last rows.
-__device__ __forceinline__ RowTile find_tile(const PagedAttnArgs& a, int G, int number, int lane) {
-  RowTile t{-1, 0, 0, 0};
-  for (int s1 = a.pool.n_seqs; s1 > 0; s1 -= 64) {
-    const int s = s1 - 1 - lane;
-    const SeqRows r = seq_rows<true>(a, max(s, 0), G);
-    const int n = s >= 0 ? (r.rows + kPreRows - 1) / kPreRows : 0;
-    const int sum = wave_scan(n);
-    const uint64_t past = __ballot(sum > number);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      t.seq = s1 - 1 - l;
-      t.begin = __builtin_amdgcn_readlane(r.begin, l);
-      t.rows = __builtin_amdgcn_readlane(r.rows, l);
-      t.first = (__builtin_amdgcn_readlane(sum, l) - 1 - number) * kPreRows;
-      break;
-    }
-    number -= __builtin_amdgcn_readlane(sum, 63);
-  }
-  return {uniform(t.seq), uniform(t.first), uniform(t.begin), uniform(t.rows)};
-}
 
 template <class T, int DH>
 __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_prefill(const PagedAttnArgs a, float* work, int parts) {
@@ -396,49 +364,6 @@ __global__ __launch_bounds__(kPreWaves * 64, DH == 64 ? 3 : 2) void k_paged_pref
   }
 }
 
-// Joins the parts of a split call.  RT threads to a row and head: a whole
-// workgroup where there are many parts, else DH / 4.
-template <class T, int DH, bool MANY>
-__global__ __launch_bounds__(256) void k_paged_join_tiles(const PagedAttnArgs a, const float* work, int parts) {
-  constexpr int RT = MANY ? 256 : DH / 4, R = 256 / RT;
-  const PagedPool& p = a.pool;
-  const int lane = threadIdx.x & 63, G = p.H / p.Hk;
-  const int per_tile = kPreRows / R;
-  const int piece = blockIdx.x % per_tile, kvh = blockIdx.x / per_tile % p.Hk, number = blockIdx.x / per_tile / p.Hk;
-  const RowTile rt = find_tile(a, G, number, lane);
-  const int r = piece * R + threadIdx.x / RT, v = rt.first + r;
-  if (rt.seq < 0 || v >= rt.rows) return;   // MANY: uniform
-  const float* from = work + (((int64_t)number * parts * p.Hk + kvh) * kPreRows + r) * (DH + 4);
-  const int64_t step = (int64_t)p.Hk * kPreRows * (DH + 4);
-  const int n = (int)from[3];   // written for every row of a call of several parts
-  if (n == 1) return;           // part 0 has written the output
-  uint16_t* out = a.out + (rt.begin + v / G) * a.out_stride + (kvh * G + v % G) * DH;
-  if constexpr (MANY) {
-    __shared__ JoinLds<DH, 256, kPreMaxParts> lds;
-    join_row<T, DH, 256>(from, step, n, lds, out);
-  } else {
-    const int d = threadIdx.x % RT * 4;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) m = fmaxf(m, from[c * step]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f, saw = 0.f;
-    pf32x4 o = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) {
-      const pf32x4 x = *(const pf32x4*)(from + c * step);
-      const float f = __builtin_amdgcn_exp2f(x[0] - ref);
-      l += x[1] * f;
-      saw += x[2];
-      o += *(const pf32x4*)(from + c * step + 4 + d) * f;
-    }
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = saw > 0.f ? o[k] * inv : 0.f;
-    *(pu32x2*)(out + d) = pack_out<T>(o);
-  }
-}
-
 PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
   const int64_t G = p.H / p.Hk, slots = (int64_t)p.max_pages << p.page_shift;
   const int64_t partial = p.n_seqs < n_rows ? p.n_seqs : n_rows;   // tiles that are not full, at most
@@ -459,11 +384,7 @@ PagedSplit paged_prefill_split(const PagedPool& p, int n_rows) {
 template <class T, int DH>
 static hipError_t prefill(const PagedAttnArgs& a, const PagedSplit& sp, void* workspace, hipStream_t s) {
   k_paged_prefill<T, DH><<<(unsigned)sp.units, kPreWaves * 64, 0, s>>>(a, (float*)workspace, sp.parts);
-  if (sp.split) {
-    const unsigned rows = (unsigned)(sp.tiles * a.pool.Hk * kPreRows);
-    if (sp.parts > 16) k_paged_join_tiles<T, DH, true><<<rows, 256, 0, s>>>(a, (const float*)workspace, sp.parts);
-    else k_paged_join_tiles<T, DH, false><<<rows * (DH / 4) / 256, 256, 0, s>>>(a, (const float*)workspace, sp.parts);
-  }
+  if (sp.split) launch_join_tiles<T, DH>(a, sp, (const float*)workspace, s);
   return hipGetLastError();
 }
 

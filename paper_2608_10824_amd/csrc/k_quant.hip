@@ -94,59 +94,6 @@ __global__ __launch_bounds__(64) void k_quant_read(const QuantReadArgs a) {
   }
 }
 
-// A wave for each row and query head: the largest score, then the sums, in double, slot by slot.
-template <class T, int DH>
-__global__ __launch_bounds__(64) void k_quant_attend(const PagedAttnArgs a, const QuantPages from) {
-  constexpr int N = DH / 64;
-  const PagedPool& p = a.pool;
-  const int row = blockIdx.x / p.H, h = blockIdx.x % p.H, G = p.H / p.Hk, kvh = h / G, lane = threadIdx.x;
-  const int slots = p.max_pages << p.page_shift;
-  int seq = row, last;
-  if (a.row_begin) {
-    seq_of_row(a, row, G, lane, seq);
-    if (seq < 0) return;   // a row of no sequence
-    last = min(max(a.row_last[row], -1), slots - 1);
-  } else {
-    last = min(max(a.row_last[row], 0), slots) - 1;
-  }
-  float q[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) q[i] = T::up(a.q[row * a.q_stride + h * DH + lane + 64 * i]);
-  const int sinks = a.window ? min(a.n_sinks, max(last - a.window + 1, 0)) : 0;
-  const int first = a.window ? max(last - a.window + 1, 0) : 0;
-  float top = -INFINITY;
-  double sum = 0, o[N] = {};
-  bool any = false;
-  for (int pass = 0; pass < 2; ++pass)
-    for (int i = 0; i < sinks + last + 1 - first; ++i) {
-      const int j = i < sinks ? i : first + i - sinks;
-      const QuantPlace at = quant_place(p, seq, j);
-      if (at.page < 0) continue;
-      const int64_t head = (int64_t)at.page * p.Hk + kvh, slot = (head << p.page_shift) + at.off;
-      const float ks = scale_of(from.k_scale[slot]), vs = scale_of(from.v_scale[slot]);
-      float s = 0.f;
-#pragma unroll
-      for (int d = 0; d < N; ++d)
-        s = fmaf(q[d], T::up((uint16_t)decoded<T, false>(from.k[slot * DH + lane + 64 * d], ks)), s);
-      s = wave_sum(s) * a.scale_log2e;
-      if (pass == 0) {
-        top = fmaxf(top, s);
-        any = true;
-        continue;
-      }
-      const float x = __builtin_amdgcn_exp2f(s - top);
-      sum += x;
-#pragma unroll
-      for (int d = 0; d < N; ++d)
-        o[d] += (double)x * T::up((uint16_t)decoded<T, false>(from.v[((head * DH + lane + 64 * d) << p.page_shift) + at.off], vs));
-    }
-#pragma unroll
-  for (int d = 0; d < N; ++d) {
-    const pu32x2 out = pack_out<T>(pf32x4{any ? (float)(o[d] / sum) : 0.f, 0, 0, 0});
-    a.out[row * a.out_stride + h * DH + lane + 64 * d] = (uint16_t)out[0];
-  }
-}
-
 #define GVC_QUANT_LAUNCH(kernel, dh, grid, ...)                                       \
   do {                                                                                \
     if ((grid) >= 1 << 26) return hipErrorInvalidConfiguration;                       \
@@ -165,9 +112,6 @@ hipError_t launch_quant_append(const PagedAppendArgs& a, const QuantPages& to, i
 }
 hipError_t launch_quant_read(const QuantReadArgs& a, int dtype, hipStream_t s) {
   GVC_QUANT_LAUNCH(k_quant_read, a.pool.dh, (int64_t)a.n_rows * a.pool.Hk, a);
-}
-hipError_t launch_quant_attend(const PagedAttnArgs& a, const QuantPages& from, int dtype, hipStream_t s) {
-  GVC_QUANT_LAUNCH(k_quant_attend, a.pool.dh, (int64_t)a.n_rows * a.pool.H, a, from);
 }
 
 }  // namespace gvc

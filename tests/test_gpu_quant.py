@@ -19,7 +19,7 @@ import torch
 from oracle import paged as op
 from oracle import quant as oq
 from tests import test_gpu_paged as paged
-from tests.test_gpu_paged import DEV, TYPES, _np, _ragged, _tiny, _u
+from tests.test_gpu_paged import DEV, TYPES, _np, _ragged, _tiled, _tiny, _u
 
 pytestmark = pytest.mark.gpu
 
@@ -61,12 +61,25 @@ class Pool(paged.Pool):
         c = self.cache
         return [x.view(torch.uint8) for x in (c.k_pages, c.k_scales, c.v_pages, c.v_scales)]
 
-    def expect(self, *args, **kw):
-        held, self.cache = self.cache, Values(self.cache, self.t)
-        try:
-            return super().expect(*args, **kw)
-        finally:
-            self.cache = held
+    def expect(self, out, q, seqs, lasts, window=0, sinks=0, scale=None):
+        """Compares attention outputs with the oracle's, row by row (the bounds of the 16-bit cache's tests)."""
+        val = Values(self.cache, self.t)
+        k, v, q, out = val.k_pages.numpy(), val.v_pages.numpy(), _np(q), _np(out)
+        scale = self.dh ** -0.5 if scale is None else scale
+        u, vmax = _u(self.t), np.abs(v[np.isfinite(v)]).max(initial=0)
+        for r, (s, last) in enumerate(zip(seqs, lasts)):
+            want, mag, top, n = op.attend_row(q[r], s, last, k, v, self.table, scale, window, sinks)
+            if n == 0:
+                assert not out[r].any(), "row %d sees nothing and is not zero" % r
+                continue
+            assert np.array_equal(np.isnan(out[r]), np.isnan(want)), "row %d: NaN" % r
+            fine, inf = np.isfinite(want), np.isinf(want)
+            assert np.array_equal(out[r][inf], want[inf]), "row %d: inf" % r
+            p = (2 * (self.dh + 8) * 2.0 ** -23 * top + (n + 64) * 2.0 ** -23 + u)[:, None]
+            with np.errstate(invalid="ignore"):
+                tol = u * np.abs(want) + mag * p * (1 + u) + _tiny(self.t) * (1 + n / 64 * vmax)
+                over = (np.abs(out[r] - want) - tol)[fine]
+            assert over.max(initial=0) <= 0, "row %d (sequence %d, last %d): %.3g over its bound" % (r, s, last, over.max())
 
 
 # ------------------------------------------------------------------- append
@@ -474,6 +487,320 @@ def test_prefill_of_one_row_is_decode():
     p = pool.cache.prefill(q, pool.ints([36, 599, 0]), pool.ints([0, 1, 2, 3]))
     pool.expect(d, q, range(3), [36, 599, 0])
     pool.expect(p, q, range(3), [36, 599, 0])
+
+
+# ------------------------------------- prefill: lists long enough for tiles of 128 rows
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv,dh,page,columns", [(56, 8, 128, 16, 0), (64, 1, 64, 32, 0), (64, 32, 64, 128, 0),
+                                                      (53, 1, 128, 64, 0), (6, 2, 128, 16, 195), (5, 1, 64, 128, 26),
+                                                      (4, 4, 64, 16, 200)])
+def test_tiles_of_ragged_rows(t, heads, kv, dh, page, columns):
+    """Whole prompts, one row, no row, chunks behind a cached prefix, rows with
+    gaps, rows in falling order; tables that hold the lengths alone, and such
+    that the slots are split."""
+    pool = Pool(51, t, kv, dh, page, [150, 1, 40, 256, 97, 66], extra_columns=columns)
+    rows = [range(150), [0], [], range(197, 256), sorted(pool.r.permutation(97)[:41]), range(65, -1, -1)]
+    _tiled(pool, sum(len(x) for x in rows), heads)
+    _ragged(pool, heads, rows)
+
+
+@pytest.mark.parametrize("t,dh,page,kv", [("bf16", 64, 16, 2), ("fp16", 128, 64, 1)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (9, 4), (64, 0), (31, 33), (130, 5), (64, 200), (300, 2)])
+def test_tiles_with_window_and_sinks(t, dh, page, kv, window, sinks):
+    pool = Pool(52, t, kv, dh, page, [333, 20, 180])
+    rows = [range(140, 333), range(20), range(0, 180, 3)]
+    heads = ((1 << 22) // (273 * kv * min(window + sinks + 64, 300)) + 1) * kv
+    _tiled(pool, 273, heads, window, sinks)
+    _ragged(pool, heads, rows, window, sinks)
+
+
+@pytest.mark.parametrize("t,dh,page", [("bf16", 128, 64), ("fp16", 64, 16), ("bf16", 64, 128), ("fp16", 128, 16)])
+def test_tiles_over_many_slots(t, dh, page):
+    """Few tiles over thousands of slots, split and joined: in up to sixteen
+    parts and in more, with and without a window, and rows that see few of them."""
+    pool = Pool(53, t, 1, dh, page, [5100])
+    _tiled(pool, 41, 21)
+    _ragged(pool, 21, [[5099, 0, 300] + list(range(5062, 5100))])
+    _tiled(pool, 90, 30, 1500, 70)
+    _ragged(pool, 30, [range(5010, 5100)], 1500, 70)
+    pool = Pool(54, t, 2, dh, page, [2000, 130, 900])
+    rows = [range(1900, 2000), range(130), [899]]
+    _tiled(pool, 231, 10)
+    _ragged(pool, 10, rows)
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_tiles_where_rows_see_nothing_or_see_each_other(columns):
+    """Empty rows among others and whole tiles of them, an action block whose
+    rows give the block's last slot, rows of no sequence before and behind."""
+    heads = 80 if columns == 0 else 6
+    pool = Pool(55, "bf16", 2, 64, 16, [256, 60], extra_columns=columns)
+    lasts = [5] * 7 + [-1, 3, -1, 49] + list(range(90)) + [99] * 30 + [-1] * 90 + [7, -9, 59] + [8] * 6
+    n = len(lasts)
+    q = pool.rows(n, heads)
+    _tiled(pool, n, heads)
+    held = torch.full((n, heads, 64), 768.0, dtype=torch.bfloat16, device=DEV)
+    out = pool.cache.prefill(q, pool.ints(lasts), pool.ints([7, n - 9, n - 6]), out=held)
+    assert (held[:7] == 768).all() and (held[n - 6:] == 768).all()
+    pool.expect(out[7:n - 6], q[7:n - 6], [0] * (n - 16) + [1] * 3, lasts[7:n - 6])
+
+
+@pytest.mark.parametrize("columns", [0, 200])
+def test_tiles_with_pages_that_do_not_exist(columns):
+    heads = 72 if columns == 0 else 6
+    pool = Pool(56, "fp16", 1, 64, 16, [256, 128, 64], extra_columns=columns)
+    c = pool.cache
+    for s, col, to in ((0, 0, -1), (0, 3, c.k_pages.shape[0]), (0, 9, -2 ** 31), (1, 2, 2 ** 31 - 1), (2, 0, -7),
+                       (2, 1, -1), (2, 2, -1), (2, 3, -1)):
+        pool.table[s, col] = to
+    c.page_table.copy_(torch.tensor(pool.table))
+    _tiled(pool, 250, heads)
+    _, out, _, _, _ = _ragged(pool, heads, [range(106, 256), range(40, 128), range(52, 64)])
+    assert not out[238:].any()
+    # a length over what the table holds ends at the table's last slot
+    last = pool.table.shape[1] * 16 - 1
+    q = pool.rows(250, heads)
+    out = c.prefill(q, pool.ints([2 ** 31 - 1, last + 1] * 125), pool.ints([0, 250, 250, 250]))
+    pool.expect(out, q, [0] * 250, [last] * 250)
+
+
+@pytest.mark.parametrize("t,heads,columns,window,sinks", [("bf16", 72, 0, 0, 0), ("fp16", 72, 0, 0, 0), ("bf16", 6, 180, 0, 0),
+                                                          ("fp16", 156, 0, 40, 4), ("bf16", 156, 200, 40, 4)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_tiles_keep_nan_and_infinities_with_the_rows_that_see_them(t, heads, columns, window, sinks, dh):
+    pool = Pool(57, t, 2, dh, 16, [256], extra_columns=columns)
+    (k, ks, v, vs), tb = pool.bytes(), pool.table
+    v[tb[0, 5], 0, 3, 7] = 0x7f                                        # slot 87
+    vs[tb[0, 8], 1, 1], v[tb[0, 8], 1, :, 1] = 253 if t == "bf16" else 140, 0
+    v[tb[0, 8], 1, 9, 1] = 0x7e                                        # slot 129: an infinity
+    k[tb[0, 9], 0, 15, 0] = 0x7f                                       # slot 159
+    vs[tb[0, 10], 1, 3] = 255                                          # slot 163
+    _tiled(pool, 256, heads, window, sinks)
+    _, out, _, _, _ = _ragged(pool, heads, [range(256)], window, sinks)
+    o, g = _np(out), heads // 2
+    assert np.isfinite(o[:87]).all() and np.isnan(o[87, :g, 3]).all() and np.isfinite(o[:159, g:, :9]).all()
+    assert np.isinf(o[129, g:, 9]).all() and np.isnan(o[159, :g]).all() and np.isnan(o[163, g:]).all()
+    if window:
+        assert np.isfinite(o[203:]).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+def test_tiles_of_steep_scores(t):
+    """The running maximum moves up and down over hundreds."""
+    pool = Pool(58, t, 1, 64, 16, [256])
+    ks = pool.bytes()[1]
+    for j in range(256):
+        ks[pool.table[0, j // 16], 0, j % 16] += j % 50 // 17
+    _tiled(pool, 256, 72)
+    _ragged(pool, 72, [range(256)], scale=4.0)
+
+
+def test_tiles_strides_scale_and_out():
+    pool = Pool(59, "bf16", 2, 128, 32, [256])
+    wide = pool.rows(256, 70)
+    q = wide[:, 4:64]
+    held = torch.full((256, 62, 128), 3.0, dtype=torch.bfloat16, device=DEV)
+    _tiled(pool, 256, 60)
+    out = pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3, out=held[:, 1:61])
+    assert (held[:, 0] == 3).all() and (held[:, 61] == 3).all()
+    pool.expect(out, q, [0] * 256, range(256), scale=0.3)
+    want = pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3)
+    assert torch.equal(pool.cache.prefill(q, pool.ints(range(256)), pool.ints([0, 256]), scale=0.3, out=q), want)
+
+
+def test_captured_tiles_replay_with_other_rows():
+    """A captured call of long lists, split over the slots: rows, bounds and
+    the table change between replays; each is bit for bit the eager result."""
+    pool = Pool(60, "bf16", 2, 64, 16, [1500, 700], spare=30)
+    c = pool.cache
+    n, heads = 400, 8
+    q, last, begin = pool.rows(n, heads), pool.ints([3] * n), pool.ints([0, 200, n])
+    _tiled(pool, n, heads)
+    graphs, outs = [], []
+    c.prefill(q, last, begin)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.prefill(q, last, begin))
+        graphs.append(g)
+    for turn, (cut, a, b) in enumerate([(200, 1499, 699), (350, 1499, 60), (10, 20, 699), (400, 1100, -1)]):
+        q.copy_(pool.rows(n, heads))
+        lasts = [max(a - cut + 1 + i, -1) for i in range(cut)] + [max(b - n + cut + 1 + i, -1) for i in range(n - cut)]
+        last.copy_(pool.ints(lasts))
+        begin.copy_(pool.ints([0, cut, n]))
+        want = c.prefill(q, last, begin)
+        if turn < 2:
+            pick = list(range(0, n, 23)) + [cut - 1, n - 1]
+            pool.expect(want[pick], q[pick], [int(i >= cut) for i in pick], [lasts[i] for i in pick])
+        for g, got in zip(graphs, outs):
+            got.fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(want, got)
+
+
+@pytest.mark.parametrize("rows,length", [(10, 50), (10, 3000), (300, 3000), (400, 3000)])
+def test_prefill_with_bounds_that_fall(rows, length):
+    """Bounds have to rise; where they do not, no row outside them is touched (nor any other memory)."""
+    pool = Pool(26, "bf16", 2, 64, 16, [length] * 4)
+    q = pool.rows(rows + 9, 4)
+    held = torch.full((rows + 9, 4, 64), 768.0, dtype=torch.bfloat16, device=DEV)
+    pool.cache.prefill(q, pool.ints([length - 1] * (rows + 9)), pool.ints([0, rows, 0, rows, rows + 7]), out=held)
+    assert (held[rows + 7:] == 768).all()
+
+
+# ------------------------------------------------------- workspaces of split calls
+def test_a_workspace_may_hold_anything():
+    """Split decodes and prefills through the C ABI, in memory that holds zeros,
+    ones, noise, another call's rest and their own: the same bits."""
+    from paper_2608_10824_amd import gvc
+    pool = Pool(61, "bf16", 2, 128, 16, [7000, 17, 2100, 0])
+    c = pool.cache
+    desc = gvc.PagedDesc(gvc.BF16, 8, 2, 128, 16, c.k_pages.shape[0], 4, c.page_table.shape[1])
+    q, lengths, begin = pool.rows(20, 8), pool.ints([7000, 17, 2100, 0]), pool.ints([0, 1, 2, 20, 20])
+    last = pool.ints([6999, 16] + list(range(2082, 2100)))
+    long_q, long_last, long_begin = pool.rows(300, 8), pool.ints(range(1800, 2100)), pool.ints([0, 0, 0, 300, 300])
+    pages = c._pages()
+    sizes = [gvc.quant_workspace(desc, False, 4), gvc.quant_workspace(desc, True, 20), gvc.quant_workspace(desc, True, 300)]
+    assert min(sizes) > 0
+    work = torch.zeros(max(sizes), dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def run():
+        outs = [torch.empty_like(x) for x in (q[:4], q, long_q)]
+        gvc.quant_decode(desc, 0.09, 0, 0, q.data_ptr(), 1024, lengths.data_ptr(), *pages, outs[0].data_ptr(), 1024,
+                         work.data_ptr(), sizes[0], stream)
+        gvc.quant_prefill(desc, 0.09, 0, 0, q.data_ptr(), 1024, last.data_ptr(), begin.data_ptr(), 20, *pages,
+                          outs[1].data_ptr(), 1024, work.data_ptr(), sizes[1], stream)
+        gvc.quant_prefill(desc, 0.09, 0, 0, long_q.data_ptr(), 1024, long_last.data_ptr(), long_begin.data_ptr(), 300,
+                          *pages, outs[2].data_ptr(), 1024, work.data_ptr(), sizes[2], stream)
+        return outs
+
+    want = run()
+    pool.expect(want[0], q[:4], range(4), [6999, 16, 2099, -1], scale=0.09)
+    pool.expect(want[1], q, [0, 1] + [2] * 18, [6999, 16] + list(range(2082, 2100)), scale=0.09)
+    noise = torch.randint(0, 256, work.shape, dtype=torch.uint8, device=DEV)
+    for fill in (None, 255, 1, noise):
+        if fill is not None:
+            work.copy_(noise) if fill is noise else work.fill_(fill)
+        for x, y in zip(want, run()):
+            assert torch.equal(x, y)
+
+
+# ------------------------------------------- values near the end of the type's range
+def _large(pool, power):
+    """The pool's values up to 2^(power + 3), all of one sign: their sums before the division are larger."""
+    v, vs = pool.bytes()[2:]
+    v.copy_(torch.where((v & 127) == 127, v, v & 127))
+    held = vs != 255
+    vs[held] = vs[held].clamp(max=119) + power   # 448 2^-8 times 2^power at most
+
+
+@pytest.mark.parametrize("power", [90, 114, 121, 126])
+def test_outputs_are_finite_where_sums_overflow(power):
+    """bf16 values to 2^127: decode (split and not, with a window) and lists of few rows give
+    the finite outputs of their formulas."""
+    lengths = [1, 40, 700, 6000, 0]
+    pool = Pool(63, "bf16", 2, 64, 16, lengths)
+    _large(pool, power)
+    q = pool.rows(5, 8, 2.0)
+    pool.expect(pool.cache.decode(q, pool.ints(lengths)), q, range(5), [n - 1 for n in lengths])
+    pool.expect(pool.cache.decode(q, pool.ints(lengths), window=300, sinks=20), q, range(5), [n - 1 for n in lengths], 300, 20)
+    _ragged(pool, 8, [[0], range(40), [699, 3], [5999], []])
+
+
+@pytest.mark.parametrize("power", [90, 114, 121, 126])
+@pytest.mark.parametrize("dh,heads,columns", [(64, 72, 0), (128, 72, 0), (64, 6, 200), (128, 6, 200)])
+def test_tiles_are_finite_where_sums_overflow(power, dh, heads, columns):
+    pool = Pool(65, "bf16", 2, dh, 16, [256], extra_columns=columns)
+    _large(pool, power)
+    _tiled(pool, 256, heads)
+    _ragged(pool, heads, [range(256)])
+
+
+# ------------------------- calls of many sequences and many heads, by the path that they take
+@pytest.mark.parametrize("seqs,heads,kv", [(64, 4, 2), (65, 6, 2), (130, 2, 1)])
+def test_decode_many_sequences(seqs, heads, kv):
+    """Ragged batches of 64 sequences and more, idle ones among them; rows of the same as a prefill."""
+    r = np.random.default_rng(41)
+    lengths = [int(n) for n in np.where(r.random(seqs) < 0.2, 0, np.exp(r.uniform(0, 7.7, seqs)))]
+    pool = Pool(41, "bf16", kv, 64, 16, lengths)
+    q = pool.rows(seqs, heads)
+    out = pool.cache.decode(q, pool.ints(lengths))
+    pool.expect(out, q, range(seqs), [n - 1 for n in lengths])
+    out = pool.cache.decode(q, pool.ints(lengths), window=333, sinks=20)
+    pool.expect(out, q, range(seqs), [n - 1 for n in lengths], 333, 20)
+    if seqs * kv <= 130:
+        rows = [[n - 1, n // 2][:int(r.integers(0, 3))] if n else [] for n in lengths]
+        _ragged(pool, heads, rows)
+
+
+@pytest.mark.parametrize("seqs,kv,length", [(64, 8, 60000), (70, 2, 30000), (3, 8, 140000)])
+def test_decode_long_sequences_on_the_same_pages(seqs, kv, length):
+    """Lengths at which chunks are hundreds of tiles; all tables name the pages of one small pool."""
+    page, n_pages = 128, 40
+    pool = Pool(42, "fp16", kv, 64, page, [page * n_pages], spare=0, extra_columns=0)
+    columns = -(-length // page)
+    pool.table = pool.r.integers(0, n_pages, (seqs, columns)).astype(np.int32)
+    c = pool.cache
+    pool.cache = c = type(c)(c.k_pages, c.k_scales, c.v_pages, c.v_scales, torch.tensor(pool.table, device=DEV), TYPES["fp16"])
+    lengths = [int(length * f) for f in np.linspace(0.6, 1, seqs)]
+    lengths[1] = 5
+    q = pool.rows(seqs, kv)
+    out = c.decode(q, pool.ints(lengths))
+    pick = [0, 1, seqs // 2, seqs - 1]
+    pool.expect(out[pick], q[pick], pick, [lengths[i] - 1 for i in pick])
+
+
+@pytest.mark.parametrize("t,dh,heads,kv", [("bf16", 64, 32, 32), ("fp16", 64, 64, 32), ("bf16", 128, 34, 34)])
+def test_units_of_many_heads_join_long_chunks_themselves(t, dh, heads, kv):
+    """4200 to 16384 slots of at least 32 key-value heads: eight long chunks and no second launch."""
+    lengths = [5400, 300, 0, 4300]
+    pool = Pool(71, t, kv, dh, 16, lengths, extra_columns=600)
+    q = pool.rows(4, heads, 2.0)
+    for _ in range(2):   # the second in memory that the first has left
+        pool.expect(pool.cache.decode(q, pool.ints(lengths)), q, range(4), [n - 1 for n in lengths])
+    pool.expect(pool.cache.decode(q, pool.ints(lengths), window=4400, sinks=40), q, range(4), [n - 1 for n in lengths], 4400, 40)
+    if 4 * kv <= 128:
+        _ragged(pool, heads, [range(5390, 5400), [299, 0], [], [4299]])
+
+
+@pytest.mark.parametrize("seqs,kv,heads,columns", [(65, 2, 40, 0), (130, 2, 40, 0), (70, 1, 12, 200)])
+def test_tiles_of_many_sequences(seqs, kv, heads, columns):
+    """More sequences than a wave has lanes, some without rows, rows of no sequence before and behind."""
+    r = np.random.default_rng(72)
+    lengths = [int(n) for n in r.integers(0, 90, seqs)]
+    lengths[0], lengths[seqs - 1] = 90, 33
+    pool = Pool(72, "bf16", kv, 64, 16, lengths, extra_columns=columns)
+    lasts, seq, begin = [5] * 3, [-1] * 3, [3]
+    for s, n in enumerate(lengths):
+        new = 0 if s % 7 == 3 else min(n, int(r.integers(0, 60)))
+        lasts += range(n - new, n)
+        seq += [s] * new
+        begin.append(len(lasts))
+    lasts, seq = lasts + [4] * 5, seq + [-1] * 5
+    n = len(lasts)
+    _tiled(pool, n, heads)
+    q = pool.rows(n, heads, 2.0)
+    held = torch.full((n, heads, 64), 768.0, dtype=torch.bfloat16, device=DEV)
+    out = pool.cache.prefill(q, pool.ints(lasts), pool.ints(begin), out=held)
+    assert (held[:3] == 768).all() and (held[n - 5:] == 768).all()
+    pick = sorted({x for s in range(seqs) for x in (begin[s], begin[s + 1] - 1) if begin[s + 1] > begin[s]})
+    pool.expect(out[pick], q[pick], [seq[i] for i in pick], [lasts[i] for i in pick])
+
+
+@pytest.mark.parametrize("length", [3000, 6000])
+def test_few_rows_of_many_sequences(length):
+    """Lists of few rows in 70 sequences, joined by their units and by a second launch, which looks a row's sequence up."""
+    r = np.random.default_rng(74)
+    lengths = [int(n) for n in r.integers(1, 100, 70)]
+    lengths[3], lengths[66] = length, length - 400
+    pool = Pool(74, "bf16", 1, 64, 16, lengths)
+    rows = [[n - 1] if s % 3 else [] for s, n in enumerate(lengths)]
+    rows[3], rows[66], rows[69] = [length - 1, 7], [length - 401, length - 402, 900], [0]
+    assert sum(len(x) for x in rows) * 8 <= 70 * 16
+    _ragged(pool, 8, rows)
 
 
 # ----------------------------------------------------------------- together
