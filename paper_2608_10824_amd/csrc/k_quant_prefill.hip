@@ -103,16 +103,19 @@ __global__ __launch_bounds__(kPreWaves * 64, 2) void k_quant_prefill(const Paged
   auto load = [&](int t, int id) {
     const int page = __builtin_amdgcn_readlane(id, 2 * wv), off = (tile_slot(t) + 16 * wv) & in_page;
     const int64_t head = (int64_t)((unsigned)page < (unsigned)p.n_pages ? page : 0) * p.Hk + kvh;
-    const uint8_t *kp = from.k + head * head_bytes + off * DH, *vp = from.v + head * head_bytes + off;
-    const uint8_t *ks = from.k_scale + (head << p.page_shift) + off, *vs = from.v_scale + (head << p.page_shift) + off;
+    const auto k = __builtin_amdgcn_make_buffer_rsrc((char*)from.k + head * head_bytes, (short)0, head_bytes, 0x00020000);
+    const auto v = __builtin_amdgcn_make_buffer_rsrc((char*)from.v + head * head_bytes, (short)0, head_bytes, 0x00020000);
+    const int page_slots = in_page + 1;
+    const auto ks = __builtin_amdgcn_make_buffer_rsrc((char*)from.k_scale + (head << p.page_shift), (short)0, page_slots, 0x00020000);
+    const auto vs = __builtin_amdgcn_make_buffer_rsrc((char*)from.v_scale + (head << p.page_shift), (short)0, page_slots, 0x00020000);
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
-      k_in[i] = *(const pu32x4*)(kp + (i * 64 + lane) * 16);
-      k_scale[i] = ks[(i * 64 + lane) / CL];
+      k_in[i] = __builtin_amdgcn_raw_buffer_load_b128(k, lane * 16, off * DH + i * 1024, 0);
+      k_scale[i] = __builtin_amdgcn_raw_buffer_load_b8(ks, lane / CL, off + i * (64 / CL), 0);
     }
 #pragma unroll
-    for (int i = 0; i < KI; ++i) v_in[i] = *(const pu32x4*)(vp + ((i * 64 + lane) << p.page_shift));
-    v_scale = *(const pu32x4*)vs;
+    for (int i = 0; i < KI; ++i) v_in[i] = __builtin_amdgcn_raw_buffer_load_b128(v, lane << p.page_shift, off + (i << (p.page_shift + 6)), 0);
+    v_scale = __builtin_amdgcn_raw_buffer_load_b128(vs, 0, off, 0);
   };
   // The loaded tile t, whose chunks' pages are `pages`, into its stage.
   auto store = [&](int t, unsigned pages) {
