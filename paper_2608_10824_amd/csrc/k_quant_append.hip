@@ -24,7 +24,21 @@ namespace gvc {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kRows = 32;      // rows of a workgroup of values, and 7 on both sides that its runs of eight may reach
+constexpr int kReadThreads = 512, kReadRows = 64;   // (32 rows to 256 threads: 41 000 rows 70 us for 66)
 constexpr int kFill = 4096;    // waves of queries and keys that a call's rows are cut into, at least
+
+// What a call reads and writes once: past the caches' least recent lines where the call is larger than
+// the last of them (21 627 rows, 488 MB, one call after another 103 us for 111; where 97 MB stay in the cache 32.2 for 31.5).
+constexpr int64_t kLastCache = 256 << 20;
+template <bool STREAM, class V>
+__device__ __forceinline__ V once(const V* from) {
+  return STREAM ? __builtin_nontemporal_load(from) : *from;
+}
+template <bool STREAM, class V>
+__device__ __forceinline__ void once(V* to, V v) {
+  if (STREAM) __builtin_nontemporal_store(v, to);
+  else *to = v;
+}
 
 // Four values times a power of two, as codes.
 __device__ __forceinline__ uint32_t encoded4(const float* x, float f) {
@@ -32,7 +46,7 @@ __device__ __forceinline__ uint32_t encoded4(const float* x, float f) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, lo, true);
 }
 
-template <class T, int DH>
+template <class T, int DH, bool STREAM>
 __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantPages& pages, int wave, int slices) {
   constexpr int GL = DH / 8, HW = 64 / GL;   // lanes of a head, heads of a wave at a time
   constexpr int kAhead = 2;                  // groups of heads that are loaded at once
@@ -68,8 +82,8 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
 #pragma unroll
       for (int s = 0; s < kAhead; ++s) {   // past the last head: it again
         const int h = min(h0 + s * slices * HW, heads - 1);
-        x0[s] = *(const pu16x4*)(src + h * DH + c0);
-        x1[s] = *(const pu16x4*)(src + h * DH + c1);
+        x0[s] = once<STREAM>((const pu16x4*)(src + h * DH + c0));
+        x1[s] = once<STREAM>((const pu16x4*)(src + h * DH + c1));
       }
 #pragma unroll
       for (int s = 0; s < kAhead; ++s) {
@@ -100,8 +114,8 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
     heads_of(slice, p.H, a.q + row * a.q_stride, a.q_norm, [&](int h, const float* u, const float* w) {
       uint16_t* to = a.q_out + row * a.q_out_stride + h * DH;
       if (h >= p.H) return;
-      *(pu32x2*)(to + c0) = pu32x2{pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3])};
-      *(pu32x2*)(to + c1) = pu32x2{pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3])};
+      once<STREAM>((pu32x2*)(to + c0), pu32x2{pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3])});
+      once<STREAM>((pu32x2*)(to + c1), pu32x2{pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3])});
     });
   // key groups go on where the query groups ended
   const int g = slice < q_groups ? (slices - (q_groups - slice) % slices) % slices : slice - q_groups;
@@ -123,7 +137,7 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
   });
 }
 
-template <class T, int DH>
+template <class T, int DH, bool STREAM>
 __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPages& pages, int block) {
   constexpr int R = kRows, LR = R + 7;   // rows in LDS: the last run of eight may reach past the workgroup's own
   constexpr int LS = DH + 8;             // bytes from row to row
@@ -137,7 +151,7 @@ __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPa
 #pragma unroll
   for (int k = 0; k < L; ++k) {   // past the last row: it again
     const int i = tid + k * kThreads, r = min(r0 + min(i / C, LR - 1), a.n_rows - 1);
-    x[k] = *(const pu32x4*)(a.vin + r * a.v_stride + h * DH + i % C * 8);
+    x[k] = once<STREAM>((const pu32x4*)(a.vin + r * a.v_stride + h * DH + i % C * 8));
   }
   // Lane i of the first wave: row r0 - 7 + i.
   if (tid < 64) {
@@ -210,23 +224,23 @@ __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPa
     }
 }
 
-template <class T, int DH>
+template <class T, int DH, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_quant_append(const PagedAppendArgs a, const QuantPages pages, int v_blocks,
                                                            int slices) {
-  if ((int)blockIdx.x < v_blocks) append_v<T, DH>(a, pages, blockIdx.x);
-  else append_qk<T, DH>(a, pages, (blockIdx.x - v_blocks) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slices);
+  if ((int)blockIdx.x < v_blocks) append_v<T, DH, STREAM>(a, pages, blockIdx.x);
+  else append_qk<T, DH, STREAM>(a, pages, (blockIdx.x - v_blocks) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slices);
 }
 
-// Reads 32 rows of one head.  Keys: DH / 16 threads to a row, 16 codes each.  Values: where sixteen
+// Reads 64 rows of one head.  Keys: DH / 16 threads to a row, 16 codes each.  Values: where sixteen
 // rows are sixteen slots in a row, a thread loads 16 bytes of one dimension, else it gathers them
 // byte by byte; they cross over to rows in LDS.
 template <class T, int DH>
-__global__ __launch_bounds__(kThreads) void k_quant_read(const QuantReadArgs a) {
-  constexpr int R = kRows, CL = DH / 16;
+__global__ __launch_bounds__(kReadThreads) void k_quant_read(const QuantReadArgs a) {
+  constexpr int R = kReadRows, CL = DH / 16;
   constexpr int LS = DH + 8;   // bytes from row to row
   __shared__ __attribute__((aligned(16))) uint8_t codes[R * LS];
   __shared__ int s_page[R], s_off[R];
-  __shared__ uint32_t s_lead, s_lone;
+  __shared__ uint64_t s_lead, s_lone;
   const PagedPool& p = a.pool;
   const int h = blockIdx.x % p.Hk, r0 = blockIdx.x / p.Hk * R, tid = threadIdx.x, lane = tid & 63;
   if (tid < 64) {
@@ -243,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void k_quant_read(const QuantReadArgs a) 
 #pragma unroll
     for (int k = 1; k < 16; ++k) run |= lead << k;
     if (lane < R) s_page[lane] = at.page, s_off[lane] = at.off;
-    if (lane == 0) s_lead = (uint32_t)lead, s_lone = (uint32_t)(here & ~run);
+    if (lane == 0) s_lead = lead, s_lone = here & ~run;
   }
   __syncthreads();
   auto slot_at = [&](int r) { return (((int64_t)s_page[r] * p.Hk + h) << p.page_shift) + s_off[r]; };
@@ -251,50 +265,43 @@ __global__ __launch_bounds__(kThreads) void k_quant_read(const QuantReadArgs a) 
     uint16_t* to = out + (int64_t)(r0 + i / CL) * stride + h * DH + i % CL * 16;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      *(pu32x4*)(to + 8 * e) = pu32x4{decoded<T, false>(c[2 * e], f), decoded<T, true>(c[2 * e], f),
-                                      decoded<T, false>(c[2 * e + 1], f), decoded<T, true>(c[2 * e + 1], f)};
+      __builtin_nontemporal_store(pu32x4{decoded<T, false>(c[2 * e], f), decoded<T, true>(c[2 * e], f),
+                                         decoded<T, false>(c[2 * e + 1], f), decoded<T, true>(c[2 * e + 1], f)}, (pu32x4*)(to + 8 * e));
   };
-  if (a.k_out)
-    for (int i = tid; i < R * CL && r0 + i / CL < a.n_rows; i += kThreads) {
-      const int r = i / CL;
-      pu32x4 c = {0, 0, 0, 0};
-      float f = 0.f;
-      if (s_page[r] >= 0) {
-        c = *(const pu32x4*)(a.pages.k + slot_at(r) * DH + i % CL * 16);
-        f = scale_of(a.pages.k_scale[slot_at(r)]);
-      }
-      put(a.k_out, a.k_stride, i, c, f);
-    }
-  if (!a.v_out) return;
-  auto page_at = [&](int r) { return a.pages.v + ((((int64_t)s_page[r] * p.Hk + h) * DH) << p.page_shift) + s_off[r]; };
-  int turn = 0;
-  for (uint32_t m = s_lead; m; m &= m - 1, ++turn) {
-    const int r = __builtin_ctz(m), d = tid % DH;
-    if (turn % (kThreads / DH) != tid / DH) continue;
-    const pu32x4 c = *(const pu32x4*)(page_at(r) + (d << p.page_shift));
-#pragma unroll
-    for (int k = 0; k < 16; ++k) codes[(r + k) * LS + d] = (uint8_t)(c[k >> 2] >> (8 * (k & 3)));
+  // The thread's key chunk and dimension of a run are under way together.
+  static_assert(R * CL <= kReadThreads && R / 16 * DH <= kReadThreads, "one chunk and one dimension of a run to a thread");
+  const bool mine = tid < R * CL && r0 + tid / CL < a.n_rows, here = mine && s_page[tid / CL] >= 0;
+  pu32x4 kc = {0, 0, 0, 0}, vc = kc;
+  float kf = 0.f, vf = 0.f;
+  if (here && a.k_out) {
+    kc = *(const pu32x4*)(a.pages.k + slot_at(tid / CL) * DH + tid % CL * 16);
+    kf = scale_of(a.pages.k_scale[slot_at(tid / CL)]);
   }
-  if (const uint32_t lone = s_lone)
+  auto page_at = [&](int r) { return a.pages.v + ((((int64_t)s_page[r] * p.Hk + h) * DH) << p.page_shift) + s_off[r]; };
+  uint64_t leads = s_lead;
+  for (int k = tid / DH; k > 0; --k) leads &= leads - 1;
+  const int run = leads ? __builtin_ctzll(leads) : -1, dim = tid % DH;
+  if (a.v_out) {
+    if (run >= 0) vc = *(const pu32x4*)(page_at(run) + (dim << p.page_shift));
+    if (here) vf = scale_of(a.pages.v_scale[slot_at(tid / CL)]);
+  }
+  if (a.k_out && mine) put(a.k_out, a.k_stride, tid, kc, kf);
+  if (!a.v_out) return;
+  if (run >= 0)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) codes[(run + k) * LS + dim] = (uint8_t)(vc[k >> 2] >> (8 * (k & 3)));
+  if (const uint64_t lone = s_lone)
     for (int b = 0; b < R; b += 16) {
       const int r = b + (tid & 15), d0 = tid >> 4;
       if (!(lone >> r & 1)) continue;
       const uint8_t* from = page_at(r) + (d0 << p.page_shift);
 #pragma unroll
-      for (int k = 0; k < DH; k += kThreads / 16) codes[r * LS + d0 + k] = from[k << p.page_shift];
+      for (int k = 0; k < DH; k += kReadThreads / 16) codes[r * LS + d0 + k] = from[k << p.page_shift];
     }
   __syncthreads();
-  for (int i = tid; i < R * CL && r0 + i / CL < a.n_rows; i += kThreads) {
-    const int r = i / CL;
-    pu32x4 c = {0, 0, 0, 0};
-    float f = 0.f;
-    if (s_page[r] >= 0) {
-      const pu32x2 lo = *(const pu32x2*)(codes + r * LS + i % CL * 16), hi = *(const pu32x2*)(codes + r * LS + i % CL * 16 + 8);
-      c = pu32x4{lo[0], lo[1], hi[0], hi[1]};
-      f = scale_of(a.pages.v_scale[slot_at(r)]);
-    }
-    put(a.v_out, a.v_stride, i, c, f);
-  }
+  if (!mine) return;
+  const pu32x2* c = (const pu32x2*)(codes + tid / CL * LS + tid % CL * 16);
+  put(a.v_out, a.v_stride, tid, here ? pu32x4{c[0][0], c[0][1], c[1][0], c[1][1]} : pu32x4{0, 0, 0, 0}, vf);
 }
 
 template <class T, int DH>
@@ -304,13 +311,16 @@ static hipError_t append(const PagedAppendArgs& a, const QuantPages& to, hipStre
   const int want = (kFill + a.n_rows - 1) / a.n_rows, slices = want < groups ? want : groups;
   const int64_t v_blocks = (int64_t)((a.n_rows + kRows - 1) / kRows) * a.pool.Hk;
   const int64_t qk_blocks = ((int64_t)a.n_rows * slices + kWaves - 1) / kWaves;
-  k_quant_append<T, DH><<<(unsigned)(v_blocks + qk_blocks), kThreads, 0, s>>>(a, to, (int)v_blocks, slices);
+  const int64_t bytes = (int64_t)a.n_rows * ((a.q_out ? 4 * a.pool.H : 0) + 6 * a.pool.Hk) * DH;
+  const unsigned grid = (unsigned)(v_blocks + qk_blocks);
+  if (bytes > kLastCache) k_quant_append<T, DH, true><<<grid, kThreads, 0, s>>>(a, to, (int)v_blocks, slices);
+  else k_quant_append<T, DH, false><<<grid, kThreads, 0, s>>>(a, to, (int)v_blocks, slices);
   return hipGetLastError();
 }
 
 template <class T, int DH>
 static hipError_t read(const QuantReadArgs& a, hipStream_t s) {
-  k_quant_read<T, DH><<<(unsigned)((int64_t)((a.n_rows + kRows - 1) / kRows) * a.pool.Hk), kThreads, 0, s>>>(a);
+  k_quant_read<T, DH><<<(unsigned)((int64_t)((a.n_rows + kReadRows - 1) / kReadRows) * a.pool.Hk), kReadThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

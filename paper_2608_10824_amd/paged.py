@@ -285,29 +285,27 @@ class QuantPagedCache(PagedCache):
             raise ValueError("pages must be float8_e4m3fn")
         if k_scales.dtype != torch.float8_e8m0fnu or v_scales.dtype != torch.float8_e8m0fnu:
             raise ValueError("scales must be float8_e8m0fnu")
-        if k_pages.dim() != 4:
+        shape = k_pages.shape
+        if len(shape) != 4:
             raise ValueError("k_pages must be [n_pages][n_kv_heads][page_size][head_dim]")
-        n_pages, kv, page, dh = k_pages.shape
+        n_pages, kv, page, dh = shape
         if v_pages.shape != (n_pages, kv, dh, page):
             raise ValueError("v_pages must be [n_pages][n_kv_heads][head_dim][page_size]")
-        if k_scales.shape != (n_pages, kv, page) or v_scales.shape != (n_pages, kv, page):
+        if k_scales.shape != shape[:3] or v_scales.shape != shape[:3]:
             raise ValueError("scales must be [n_pages][n_kv_heads][page_size]")
         if page_table.dtype != torch.int32 or page_table.dim() != 2:
             raise ValueError("page_table must be int32 [n_seqs][max_pages]")
-        index = k_pages.get_device()
-        for t in (k_pages, k_scales, v_pages, v_scales):
-            if t.requires_grad:
-                raise ValueError("pages must not require a gradient")
-            if not t.is_contiguous():
-                raise ValueError("pages, scales and page table must be contiguous")
-            if t.get_device() != index:
-                raise ValueError("pages, scales and page table must be on one GPU")
-        if not page_table.is_contiguous():
-            raise ValueError("pages, scales and page table must be contiguous")
-        if index < 0 or page_table.get_device() != index:
-            raise ValueError("pages, scales and page table must be on one GPU")
+        if k_pages.requires_grad or k_scales.requires_grad or v_pages.requires_grad or v_scales.requires_grad:
+            raise ValueError("pages and scales must not require a gradient")
         if forward_ad._current_level >= 0:
             _no_tangents(k_pages, k_scales, v_pages, v_scales)
+        if not (k_pages.is_contiguous() and k_scales.is_contiguous() and v_pages.is_contiguous() and
+                v_scales.is_contiguous() and page_table.is_contiguous()):
+            raise ValueError("pages, scales and page table must be contiguous")
+        index = k_pages.get_device()
+        if index < 0 or not (k_scales.get_device() == v_pages.get_device() == v_scales.get_device() ==
+                             page_table.get_device() == index):
+            raise ValueError("pages, scales and page table must be on one GPU")
         self.k_scales, self.v_scales = k_scales, v_scales
         self._hold(k_pages, v_pages, page_table, dtype, index, True)
 
