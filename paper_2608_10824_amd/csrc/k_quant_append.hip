@@ -227,8 +227,9 @@ __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPa
 template <class T, int DH, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_quant_append(const PagedAppendArgs a, const QuantPages pages, int v_blocks,
                                                            int slices) {
-  if ((int)blockIdx.x < v_blocks) append_v<T, DH, STREAM>(a, pages, blockIdx.x);
-  else append_qk<T, DH, STREAM>(a, pages, (blockIdx.x - v_blocks) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slices);
+  const int qk = gridDim.x - v_blocks;   // queries and keys first: 98 us for 103 (21 627 rows), 28.3 for 31.3 (2368)
+  if ((int)blockIdx.x >= qk) append_v<T, DH, STREAM>(a, pages, blockIdx.x - qk);
+  else append_qk<T, DH, STREAM>(a, pages, blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slices);
 }
 
 // Reads 64 rows of one head.  Keys: DH / 16 threads to a row, 16 codes each.  Values: where sixteen

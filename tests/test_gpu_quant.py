@@ -217,6 +217,32 @@ def test_append_nothing():
     assert q.shape == (0, 4, 64)
 
 
+def test_a_long_append_is_its_parts():
+    """A call that passes more than the last cache holds, in one and in three: the same bits everywhere."""
+    from paper_2608_10824_amd.paged import QuantPagedCache
+    heads, kv, dh, page, n = 32, 8, 128, 32, 13001
+    assert n * (4 * heads + 6 * kv) * dh > 256 << 20 and n // 3 * (4 * heads + 6 * kv) * dh < 256 << 20
+    g = torch.Generator(device=DEV).manual_seed(86)
+    x = torch.randn(n, heads + 2 * kv, dh, generator=g, device=DEV).to(torch.bfloat16)
+    q, k, v = x.split([heads, kv, kv], dim=1)
+    gain = torch.randn(dh, generator=g, device=DEV).to(torch.bfloat16)
+    columns = -(-n // page) + 1
+    caches = [QuantPagedCache.empty(columns, page, kv, dh, 1, columns, device=DEV) for _ in range(2)]
+    for c in caches:
+        c.page_table.copy_(torch.randperm(columns, generator=torch.Generator().manual_seed(3))[None])
+    seq = torch.zeros(n, dtype=torch.int32, device=DEV)
+    slot = torch.arange(7, n + 7, dtype=torch.int32, device=DEV)
+    whole = caches[0].append(q, k, v, seq, slot, q_norm=gain, k_norm=gain)
+    for a, b in ((0, 4333), (4333, 8600), (8600, n)):
+        part = caches[1].append(q[a:b], k[a:b], v[a:b], seq[a:b], slot[a:b], q_norm=gain, k_norm=gain)
+        assert torch.equal(whole[a:b], part)
+    for name in ("k_pages", "k_scales", "v_pages", "v_scales"):
+        assert torch.equal(*(getattr(c, name).view(torch.uint8) for c in caches)), name
+    for a, b in zip(*(c.read(seq, slot) for c in caches)):
+        assert torch.equal(a, b)
+    assert (caches[0].read(seq, slot)[1].float() - v.float()).abs().max() <= 2.0 ** -4 * v.float().abs().max()
+
+
 @pytest.mark.parametrize("t", ["bf16", "fp16"])
 @pytest.mark.parametrize("dh", [64, 128])
 def test_append_sizes_and_borders(t, dh):
