@@ -480,7 +480,8 @@ int32_t gvc_paged_check(const gvc_paged_desc* desc, const int32_t* page_table, c
  * 2^127 in bf16) become that one; NaN and infinities become NaN codes and do not count for
  * the scale.  So rows that were read from a cache keep their values when they are
  * appended without norm and rotation.  q_out gets q with norm and rotation in 16 bits.
- * Rows, limits and errors as in gvc_paged_append. */
+ * Rows, limits and errors as in gvc_paged_append; where two rows of one call name the same
+ * slot, the codes of one may be left with the scale of the other. */
 int32_t gvc_quant_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* row_seq,
                          const int32_t* row_slot, int32_t n_rows, void* k_pages, void* k_scales, void* v_pages,

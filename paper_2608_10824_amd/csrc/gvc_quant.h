@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t decoded<Fp16, true>(uint32_t w, float scale)
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true));
 }
 
-// The largest code that the 16-bit type holds, with the least scale that a value past it has.
+// The largest value of a code that the 16-bit type holds (240 times a power of two: the next one, 256 times it, is past the type).
 template <class T>
 struct QuantMost;
 template <>

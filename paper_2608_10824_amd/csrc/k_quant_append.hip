@@ -3,10 +3,11 @@
 //
 // The scale of a head is 2^e with the least e for which its largest magnitude is
 // at most 448 * 2^e (from the bits of that magnitude), its codes are the values divided by it,
-// which is exact, rounded once.  A rotated key is not rounded to 16 bits before.  The
-// angle is taken in full turns in double precision and reduced to [-1/2, 1/2];
-// what fp32 cuts from it then is made good in first order, so sine and cosine are off by
-// little more than their own rounding.
+// which is exact, rounded once.  A key's norm and rotation are computed in double and
+// not rounded before (narrowed), so its codes are those of the exact key unless that is within
+// 2^-40 of half way between two codes, where 32 bits would take the other one in one value of two million.  (That
+// takes 1% of a long call of few key-value heads, 9% where every head has one.)  Queries are computed in 32 bits.
+// Angles are taken in full turns and reduced to [-1/2, 1/2].
 //
 // Everything is read and written once, so HBM bounds long calls and launch and
 // load latency short ones.  One launch of append has two kinds of workgroups, as k_paged_append.hip:
@@ -17,8 +18,16 @@
 //    codes into LDS; where eight rows fill eight slots in a row, a lane writes 8 bytes of one
 //    dimension, rows that stand alone are written byte by byte, neighbouring lanes
 //    taking neighbouring rows.
+//
+// Measured (bf16, 128 to a head): append of 21 627 rows of whole prompts, 32 heads on 8, norm and three axes 99 us,
+// 488 MB at 4.9 TB/s, a copy's rate; of 2368 rows of 16 sequences, about every second slot, 32 heads 31 us, 3.1 TB/s
+// (10 us of it bytes of V that stand alone); one row 6.9 us.  Two or four heads of values to a workgroup, kinds of
+// workgroups in turns: 5 to 10% slower.  Read of 41 000 rows of 8 heads, fp16, 64 us, 303 MB at 4.8 TB/s, of every second
+// slot 34 us (stores that stay in the caches 47); of 282 rows of 32 heads 5.1 us.
 #include "gvc_kernels.h"
 #include "gvc_quant.h"
+
+#include <type_traits>
 
 namespace gvc {
 
@@ -46,10 +55,64 @@ __device__ __forceinline__ uint32_t encoded4(const float* x, float f) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * f, x[3] * f, lo, true);
 }
 
+// Sine and cosine of t full turns, |t| <= 1/2: a quarter turn at most from a multiple of one, by Taylor's
+// series to x^13 and x^14 (off by at most 2^-45).
+__device__ __forceinline__ void sine_cosine(double t, double& sine, double& cosine) {
+  const double q = rint(4 * t), x = (t - 0.25 * q) * 6.283185307179586477, y = x * x;
+  double s = fma(y, 1. / 6227020800, -1. / 39916800), c = fma(y, -1. / 87178291200, 1. / 479001600);
+  s = fma(y, s, 1. / 362880), c = fma(y, c, -1. / 3628800);
+  s = fma(y, s, -1. / 5040), c = fma(y, c, 1. / 40320);
+  s = fma(y, s, 1. / 120), c = fma(y, c, -1. / 720);
+  s = fma(y, s, -1. / 6), c = fma(y, c, 1. / 24);
+  s = fma(x * y, s, x), c = fma(y, fma(y, c, -0.5), 1.);
+  const int i = (int)q;
+  sine = i & 1 ? c : s;
+  cosine = i & 1 ? s : c;
+  if (i & 2) sine = -sine;             // q of 2, -2 and -1
+  if ((i + 1) & 2) cosine = -cosine;   // q of 1, 2 and -2
+}
+
+// The sum over aligned groups of N lanes.
+template <int CTRL>
+__device__ __forceinline__ double other_lane(double v) {
+  const uint64_t x = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int N>
+__device__ __forceinline__ double sum_of_group(double v) {
+  v += other_lane<kDppXor1>(v);
+  v += other_lane<kDppXor2>(v);
+  v += other_lane<kDppHalfMirror>(v);
+  if constexpr (N == 16) v += other_lane<kDppMirror>(v);
+  return v;
+}
+template <int N>
+__device__ __forceinline__ float sum_of_group(float v) {
+  return group_sum<N>(v);
+}
+
+// 1 / sqrt(x).  In double one Newton step from the instruction's estimate (2^-24 at most): off by 2^-46.
+__device__ __forceinline__ float inverse_root(float x) { return 1.f / sqrtf(x); }
+__device__ __forceinline__ double inverse_root(double x) {
+  const double r = __builtin_amdgcn_rsq(x);
+  return x > 0 && x < INFINITY ? r * fma(-0.5 * x * r, r, 1.5) : r;
+}
+
+// x in 32 bits.  A double is cut to 21 bits, the last of them set where something was cut off, so that
+// rounding the result to a few bits, or comparing it with a number of a few bits, is as exact as with x.
+__device__ __forceinline__ float narrowed(float x) { return x; }
+__device__ __forceinline__ float narrowed(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint64_t top = (b >> 32) | min((uint32_t)b, 1u);
+  return (float)__builtin_bit_cast(double, top << 32);
+}
+
 template <class T, int DH, bool STREAM>
 __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantPages& pages, int wave, int slices) {
   constexpr int GL = DH / 8, HW = 64 / GL;   // lanes of a head, heads of a wave at a time
-  constexpr int kAhead = 2;                  // groups of heads that are loaded at once
+  constexpr int kAhead = 2, kAheadK = 1;     // groups of heads that are loaded at once, of queries and of keys
   const PagedPool& p = a.pool;
   const int row = wave / slices, slice = wave % slices;
   if (row >= a.n_rows) return;
@@ -58,82 +121,88 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
   const int c0 = turned ? 4 * j : 8 * j, c1 = turned ? a.n_pairs + 4 * j : c0 + 4;
   const int slot = a.row_slot[row];
   const QuantPlace at = quant_place(p, a.row_seq[row], slot);
-  float cs[4], sn[4];
+  double cs[4] = {}, sn[4] = {};
   if (turned) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int pair = c0 + i, axis = pair < a.end0 ? 0 : pair < a.end1 ? 1 : 2;
       const int pos = a.positions ? a.positions[axis * a.position_stride + row] : slot;
-      double t = (double)pos * a.turns[pair];
-      t = 2 * (t - rint(t));
-      const float half = (float)t, rest = (float)(t - (double)half) * 3.14159274f;
-      float s, c;
-      sincospif(half, &s, &c);
-      sn[i] = fmaf(c, rest, s);
-      cs[i] = fmaf(-s, rest, c);
+      const double t = (double)pos * a.turns[pair];
+      sine_cosine(t - rint(t), sn[i], cs[i]);
     }
   }
-  // groups g0, g0 + slices, .. of the row's heads from `src`, each handed to `put` with its two chunks
-  auto heads_of = [&](int g0, int heads, const uint16_t* src, const uint16_t* gain, auto put) {
+  // groups g0, g0 + slices, .. of the row's heads from `src`, AHEAD loaded at once, computed in the sines' type, each
+  // handed to `put` with its two chunks
+  auto heads_of = [&](auto ahead, const auto& sine, const auto& cosine, int g0, int heads, const uint16_t* src,
+                      const uint16_t* gain, auto put) {
+    constexpr int AHEAD = decltype(ahead)::value;
+    typedef typename std::remove_const<typename std::remove_reference<decltype(sine[0])>::type>::type Real;
     pu16x4 w0 = {0, 0, 0, 0}, w1 = w0;
     if (gain) w0 = *(const pu16x4*)(gain + c0), w1 = *(const pu16x4*)(gain + c1);
-    for (int h0 = g0 * HW + lane / GL; h0 - lane / GL < heads; h0 += slices * HW * kAhead) {
-      pu16x4 x0[kAhead], x1[kAhead];
+    for (int h0 = g0 * HW + lane / GL; h0 - lane / GL < heads; h0 += slices * HW * AHEAD) {
+      pu16x4 x0[AHEAD], x1[AHEAD];
 #pragma unroll
-      for (int s = 0; s < kAhead; ++s) {   // past the last head: it again
+      for (int s = 0; s < AHEAD; ++s) {   // past the last head: it again
         const int h = min(h0 + s * slices * HW, heads - 1);
         x0[s] = once<STREAM>((const pu16x4*)(src + h * DH + c0));
         x1[s] = once<STREAM>((const pu16x4*)(src + h * DH + c1));
       }
 #pragma unroll
-      for (int s = 0; s < kAhead; ++s) {
-        float u[4], w[4];
+      for (int s = 0; s < AHEAD; ++s) {
+        Real u[4], w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = T::up(x0[s][i]), w[i] = T::up(x1[s][i]);
         if (gain) {
-          float ss = 0.f;
+          Real ss = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) ss += u[i] * u[i] + w[i] * w[i];
-          const float r = 1.f / sqrtf(group_sum<GL>(ss) * (1.f / DH) + a.eps);
+          const Real r = inverse_root(sum_of_group<GL>(ss) * (Real)(1.f / DH) + (Real)a.eps);
 #pragma unroll
           for (int i = 0; i < 4; ++i) u[i] = u[i] * r * T::up(w0[i]), w[i] = w[i] * r * T::up(w1[i]);
         }
         if (turned)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float x = u[i], y = w[i];
-            u[i] = x * cs[i] - y * sn[i];
-            w[i] = y * cs[i] + x * sn[i];
+            const Real x = u[i], y = w[i];
+            u[i] = x * cosine[i] - y * sine[i];
+            w[i] = y * cosine[i] + x * sine[i];
           }
         put(h0 + s * slices * HW, u, w);
       }
     }
   };
-  const int q_groups = a.q_out ? (p.H + HW - 1) / HW : 0;
-  if (slice < q_groups)
-    heads_of(slice, p.H, a.q + row * a.q_stride, a.q_norm, [&](int h, const float* u, const float* w) {
-      uint16_t* to = a.q_out + row * a.q_out_stride + h * DH;
-      if (h >= p.H) return;
-      once<STREAM>((pu32x2*)(to + c0), pu32x2{pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3])});
-      once<STREAM>((pu32x2*)(to + c1), pu32x2{pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3])});
-    });
-  // key groups go on where the query groups ended
-  const int g = slice < q_groups ? (slices - (q_groups - slice) % slices) % slices : slice - q_groups;
-  heads_of(g, p.Hk, a.kin + row * a.k_stride, a.k_norm, [&](int h, float* u, float* w) {
-    float most = 0.f;
+  // keys first: what they need in double is not kept for the queries
+  const int k_groups = (p.Hk + HW - 1) / HW;
+  if (slice < k_groups)
+    heads_of(std::integral_constant<int, kAheadK>{}, sn, cs, slice, p.Hk, a.kin + row * a.k_stride, a.k_norm,
+             [&](int h, const double* u, const double* w) {
+      float x[4], y[4], most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      u[i] = bounded<T>(u[i]);
-      w[i] = bounded<T>(w[i]);
-      most = fmaxf(most, fmaxf(counted(u[i]), counted(w[i])));
-    }
-    const int code = scale_code(group_max<GL>(most));
-    if (h >= p.Hk || at.page < 0) return;
-    const int64_t to = (((int64_t)at.page * p.Hk + h) << p.page_shift) + at.off;
-    const float f = inverse_scale(code);
-    *(uint32_t*)(pages.k + to * DH + c0) = encoded4(u, f);
-    *(uint32_t*)(pages.k + to * DH + c1) = encoded4(w, f);
-    if (j == 0) pages.k_scale[to] = (uint8_t)code;
+      for (int i = 0; i < 4; ++i) {
+        x[i] = bounded<T>(narrowed(u[i]));
+        y[i] = bounded<T>(narrowed(w[i]));
+        most = fmaxf(most, fmaxf(counted(x[i]), counted(y[i])));
+      }
+      const int code = scale_code(group_max<GL>(most));
+      if (h >= p.Hk || at.page < 0) return;
+      const int64_t to = (((int64_t)at.page * p.Hk + h) << p.page_shift) + at.off;
+      const float f = inverse_scale(code);
+      *(uint32_t*)(pages.k + to * DH + c0) = encoded4(x, f);
+      *(uint32_t*)(pages.k + to * DH + c1) = encoded4(y, f);
+      if (j == 0) pages.k_scale[to] = (uint8_t)code;
+    });
+  if (!a.q_out) return;
+  float cos_q[4], sin_q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) cos_q[i] = (float)cs[i], sin_q[i] = (float)sn[i];
+  // query groups go on where the key groups ended
+  const int g = slice < k_groups ? (slices - (k_groups - slice) % slices) % slices : slice - k_groups;
+  heads_of(std::integral_constant<int, kAhead>{}, sin_q, cos_q, g, p.H, a.q + row * a.q_stride, a.q_norm,
+           [&](int h, const float* u, const float* w) {
+    uint16_t* to = a.q_out + row * a.q_out_stride + h * DH;
+    if (h >= p.H) return;
+    once<STREAM>((pu32x2*)(to + c0), pu32x2{pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3])});
+    once<STREAM>((pu32x2*)(to + c1), pu32x2{pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3])});
   });
 }
 
@@ -224,8 +293,9 @@ __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPa
     }
 }
 
+// (Seven waves to a SIMD: 72 registers for 74, 98.9 us for 100.9, 21 627 rows.)
 template <class T, int DH, bool STREAM>
-__global__ __launch_bounds__(kThreads) void k_quant_append(const PagedAppendArgs a, const QuantPages pages, int v_blocks,
+__global__ __launch_bounds__(kThreads, 7) void k_quant_append(const PagedAppendArgs a, const QuantPages pages, int v_blocks,
                                                            int slices) {
   const int qk = gridDim.x - v_blocks;   // queries and keys first: 98 us for 103 (21 627 rows), 28.3 for 31.3 (2368)
   if ((int)blockIdx.x >= qk) append_v<T, DH, STREAM>(a, pages, blockIdx.x - qk);

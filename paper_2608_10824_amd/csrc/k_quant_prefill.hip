@@ -9,6 +9,13 @@
 // scale.  A dimension of V has a byte for each of the wave's 16 slots, whose scales are
 // the same in all lanes (scalar registers): a pair is converted twice, with either slot's scale, and a
 // half taken of both.  What no row sees is made zero on the way.
+//
+// Measured: 6000 rows behind 3000 slots, 32 heads of 128 on 8, bf16, 613 to 625 us, 945 to 962 TFLOP/s of the
+// products that rows see; heads of 64 368 us, 802 TFLOP/s; 16 chunks with a window of 600, heads of 64, fp16, 33 us.
+// The softmax and the products take turns as in the 16-bit kernel (matrix cores busy 42%, vector units 50% of the time); the
+// conversions add a quarter to the vector instructions, and their way through LDS from registers takes as long
+// as reading the operands (a write of 1 KiB 16 cycles for the read's 4).  Conversions beside the first product or between the two took
+// the same time; 8 waves, which share them among 256 rows, 0 to 4% less for long lists and up to 50% more for shorter ones.
 #include "gvc_paged_tiles.h"
 #include "gvc_quant.h"
 #include "gvc_sync.h"
