@@ -64,8 +64,9 @@ class Pool(paged.Pool):
         c = self.cache
         return [x.view(torch.uint8) for x in (c.k_pages, c.k_scales, c.v_pages, c.v_scales)]
 
-    def expect(self, out, q, seqs, lasts, window=0, sinks=0, scale=None):
-        """Compares attention outputs with the oracle's, row by row (the bounds of the 16-bit cache's tests)."""
+    def expect(self, out, q, seqs, lasts, window=0, sinks=0, scale=None, least=0.0):
+        """Compares attention outputs with the oracle's, row by row (the bounds of the 16-bit cache's tests,
+        and `least` more)."""
         val = Values(self.cache, self.t)
         k, v, q, out = val.k_pages.numpy(), val.v_pages.numpy(), _np(q), _np(out)
         scale = self.dh ** -0.5 if scale is None else scale
@@ -80,7 +81,7 @@ class Pool(paged.Pool):
             assert np.array_equal(out[r][inf], want[inf]), "row %d: inf" % r
             p = (2 * (self.dh + 8) * 2.0 ** -23 * top + (n + 64) * 2.0 ** -23 + u)[:, None]
             with np.errstate(invalid="ignore"):
-                tol = u * np.abs(want) + mag * p * (1 + u) + _tiny(self.t) * (1 + n / 64 * vmax)
+                tol = u * np.abs(want) + mag * p * (1 + u) + _tiny(self.t) * (1 + n / 64 * vmax) + least
                 over = (np.abs(out[r] - want) - tol)[fine]
             assert over.max(initial=0) <= 0, "row %d (sequence %d, last %d): %.3g over its bound" % (r, s, last, over.max())
 
@@ -1000,3 +1001,48 @@ def test_pool_over_four_gib():
     begin = torch.tensor([0, 2, 3], dtype=torch.int32, device=DEV)
     qp = q[:3].contiguous()
     assert torch.equal(c.prefill(qp, last, begin), small.prefill(qp, last, begin))
+
+
+@pytest.mark.parametrize("t,size", [("bf16", 124), ("fp16", 13)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_heads_below_the_types_normal_range(t, size, dh):
+    """Keys and values that the type holds with few bits (rounded, some to zero), under queries and a scale
+    that make their scores count.  Outputs in bf16 are as small: rounded to steps of 2^-133 (off by 2^-134), of a sum
+    in 32 bits whose 300 products and divisions are rounded to steps of 2^-149 (off by 600 * 2^-150 in all, for a sum of
+    weights of 1 or more), which is less than 2^-133 together.  (The fp16 bounds hold fp16's steps already.)"""
+    least = 2.0 ** -133 if t == "bf16" else 0.0
+    pool = Pool(81, t, 2, dh, 16, [300, 40])
+    k, ks, v, vs = pool.bytes()
+    low = 1 if t == "bf16" else 103   # 2^-126, 2^-24
+    for x in (ks, vs):
+        x.copy_(torch.tensor(pool.r.integers(low, low + 4, tuple(x.shape)).astype(np.uint8)))
+    for x in (k, v):
+        x.copy_(torch.tensor(pool.r.integers(0, 0x48, tuple(x.shape)).astype(np.uint8)))
+    q = pool.rows(2, 4, 2.0 ** size)
+    pool.expect(pool.cache.decode(q, pool.ints([300, 40]), scale=64.0), q, [0, 1], [299, 39], scale=64.0, least=least)
+    rows = [(0, j) for j in range(200, 300)] + [(1, j) for j in range(40)]
+    for heads in (4, 20):
+        q = pool.rows(140, heads, 2.0 ** size)
+        out = pool.cache.prefill(q, pool.ints([j for _, j in rows]), pool.ints([0, 100, 140]), scale=64.0)
+        pool.expect(out, q, [s for s, _ in rows], [j for _, j in rows], scale=64.0, least=least)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_nan_and_overflow_in_sight_of_fp16(dh):
+    """A NaN code, a NaN scale and values past the type's range, seen by some rows."""
+    pool = Pool(82, "fp16", 1, dh, 16, [40] * 4)
+    (k, ks, v, vs), t = pool.bytes(), pool.table
+    vs[t[0, 1], 0, 4], v[t[0, 1], 0, :, 4], v[t[0, 1], 0, 3, 4] = 135, 0, 0x7e   # 448 * 2^8
+    v[t[1, 2], 0, 5, 1] = 0x7f
+    k[t[2, 0], 0, 7, 0] = 0xff
+    vs[t[3, 0], 0, 9] = 255
+    q = pool.rows(4, 2)
+    out = pool.cache.decode(q, pool.ints([40] * 4))
+    assert torch.isinf(out[0, :, 3]).all() and torch.isnan(out[1, :, 5]).all() and torch.isnan(out[2:]).all()
+    pool.expect(out, q, range(4), [39] * 4)
+    lasts = [j for _ in range(4) for j in range(40)]
+    for heads in (2, 60):
+        q = pool.rows(160, heads)
+        out = pool.cache.prefill(q, pool.ints(lasts), pool.ints([0, 40, 80, 120, 160]))
+        assert torch.isinf(out[20:40, :, 3]).all() and torch.isfinite(out[:20]).all()
+        pool.expect(out, q, [s for s in range(4) for _ in range(40)], lasts)
