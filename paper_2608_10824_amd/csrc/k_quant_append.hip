@@ -4,7 +4,7 @@
 // The scale of a head is 2^e with the least e for which its largest magnitude is
 // at most 448 * 2^e (from the bits of that magnitude), its codes are the values divided by it,
 // which is exact, rounded once.  A key's norm and rotation are computed in double and
-// not rounded before (narrowed), so its codes are those of the exact key unless that is within
+// not rounded before (high_word), so its codes are those of the exact key unless that is within
 // 2^-40 of half way between two codes, where 32 bits would take the other one in one value of two million.  (That
 // takes 1% of a long call of few key-value heads, 9% where every head has one.)  Queries are computed in 32 bits.
 // Angles are taken in full turns and reduced to [-1/2, 1/2].
@@ -48,6 +48,8 @@ __device__ __forceinline__ void once(V* to, V v) {
   if (STREAM) __builtin_nontemporal_store(v, to);
   else *to = v;
 }
+
+constexpr float kMostCode = 240.f;   // QuantMost is this times a power of two
 
 // Four values times a power of two, as codes.
 __device__ __forceinline__ uint32_t encoded4(const float* x, float f) {
@@ -100,13 +102,36 @@ __device__ __forceinline__ double inverse_root(double x) {
   return x > 0 && x < INFINITY ? r * fma(-0.5 * x * r, r, 1.5) : r;
 }
 
-// x in 32 bits.  A double is cut to 21 bits, the last of them set where something was cut off, so that
-// rounding the result to a few bits, or comparing it with a number of a few bits, is as exact as with x.
-__device__ __forceinline__ float narrowed(float x) { return x; }
-__device__ __forceinline__ float narrowed(double x) {
+// Keys are quantised from doubles: a gain or a rotation can carry 16-bit values past the ends of a float's range, where it
+// would be infinite or lose bits.  They are scaled in double too, and only then become floats.
+
+// The high word of a double, its last bit set where the low one is not zero: rounding that to a few bits, or
+// comparing it with a number of a few bits, is as exact as with the double.
+__device__ __forceinline__ uint32_t high_word(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const uint64_t top = (b >> 32) | min((uint32_t)b, 1u);
-  return (float)__builtin_bit_cast(double, top << 32);
+  return (uint32_t)(b >> 32) | min((uint32_t)b, 1u);
+}
+// The size of a word's double where that is finite, else 0.
+__device__ __forceinline__ uint32_t counted_word(uint32_t w) {
+  const uint32_t size = w & 0x7fffffff;
+  return size < 0x7ff00000 ? size : 0;
+}
+// As scale_code(), of the word of a head's largest magnitude.
+__device__ __forceinline__ int scale_code_of_word(uint32_t most) {
+  return max((int)(most >> 20) - 1023 + 127 - 8 + ((most & 0xfffff) > 0xc0000 ? 1 : 0), 1);
+}
+// Doubles, given by their words, divided by their scale.
+__device__ __forceinline__ float scaled(uint32_t w, int scale_code) {
+  return (float)__builtin_ldexp(__builtin_bit_cast(double, (uint64_t)w << 32), 127 - scale_code);
+}
+// The largest over aligned groups of N lanes.
+template <int N>
+__device__ __forceinline__ uint32_t max_of_group(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppXor1, 0xF, 0xF, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppXor2, 0xF, 0xF, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppHalfMirror, 0xF, 0xF, false));
+  if constexpr (N == 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppMirror, 0xF, 0xF, false));
+  return v;
 }
 
 template <class T, int DH, bool STREAM>
@@ -116,7 +141,7 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
   const PagedPool& p = a.pool;
   const int row = wave / slices, slice = wave % slices;
   if (row >= a.n_rows) return;
-  const int lane = threadIdx.x & 63, j = lane & (GL - 1);
+  const int sub = (threadIdx.x & 63) / GL, j = threadIdx.x & (GL - 1);   // one of the wave's heads, a lane of it
   const bool turned = 4 * j < a.n_pairs;
   const int c0 = turned ? 4 * j : 8 * j, c1 = turned ? a.n_pairs + 4 * j : c0 + 4;
   const int slot = a.row_slot[row];
@@ -139,7 +164,8 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
     typedef typename std::remove_const<typename std::remove_reference<decltype(sine[0])>::type>::type Real;
     pu16x4 w0 = {0, 0, 0, 0}, w1 = w0;
     if (gain) w0 = *(const pu16x4*)(gain + c0), w1 = *(const pu16x4*)(gain + c1);
-    for (int h0 = g0 * HW + lane / GL; h0 - lane / GL < heads; h0 += slices * HW * AHEAD) {
+    for (int g = g0; g * HW < heads; g += slices * AHEAD) {
+      const int h0 = g * HW + sub;
       pu16x4 x0[AHEAD], x1[AHEAD];
 #pragma unroll
       for (int s = 0; s < AHEAD; ++s) {   // past the last head: it again
@@ -176,20 +202,30 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
   if (slice < k_groups)
     heads_of(std::integral_constant<int, kAheadK>{}, sn, cs, slice, p.Hk, a.kin + row * a.k_stride, a.k_norm,
              [&](int h, const double* u, const double* w) {
-      float x[4], y[4], most = 0.f;
+      constexpr uint32_t kMost = (uint32_t)(__builtin_bit_cast(uint64_t, (double)QuantMost<T>::value) >> 32);
+      uint32_t x[4], y[4], most = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = bounded<T>(narrowed(u[i]));
-        y[i] = bounded<T>(narrowed(w[i]));
-        most = fmaxf(most, fmaxf(counted(x[i]), counted(y[i])));
+        x[i] = high_word(u[i]);
+        y[i] = high_word(w[i]);
+        most = max(most, max(counted_word(x[i]), counted_word(y[i])));
       }
-      const int code = scale_code(group_max<GL>(most));
+      most = max_of_group<GL>(most);
       if (h >= p.Hk || at.page < 0) return;
       const int64_t to = (((int64_t)at.page * p.Hk + h) << p.page_shift) + at.off;
-      const float f = inverse_scale(code);
-      *(uint32_t*)(pages.k + to * DH + c0) = encoded4(x, f);
-      *(uint32_t*)(pages.k + to * DH + c1) = encoded4(y, f);
-      if (j == 0) pages.k_scale[to] = (uint8_t)code;
+      const int code = scale_code_of_word(min(most, kMost));
+      float xs[4], ys[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xs[i] = scaled(x[i], code), ys[i] = scaled(y[i], code);
+      if (__builtin_expect(most > kMost, 0))   // finite values past the largest code
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (fabsf(xs[i]) < INFINITY) xs[i] = fminf(fmaxf(xs[i], -kMostCode), kMostCode);
+          if (fabsf(ys[i]) < INFINITY) ys[i] = fminf(fmaxf(ys[i], -kMostCode), kMostCode);
+        }
+      *(uint32_t*)(pages.k + to * DH + c0) = encoded4(xs, 1.f);
+      *(uint32_t*)(pages.k + to * DH + c1) = encoded4(ys, 1.f);
+      if (c0 == 0) pages.k_scale[to] = (uint8_t)code;
     });
   if (!a.q_out) return;
   float cos_q[4], sin_q[4];

@@ -1046,3 +1046,48 @@ def test_nan_and_overflow_in_sight_of_fp16(dh):
         out = pool.cache.prefill(q, pool.ints(lasts), pool.ints([0, 40, 80, 120, 160]))
         assert torch.isinf(out[20:40, :, 3]).all() and torch.isfinite(out[:20]).all()
         pool.expect(out, q, [s for s in range(4) for _ in range(40)], lasts)
+
+
+# --------------------------------------------------- append at the ends of 32 bits
+def _keys(pool, k, positions, pairs=None, gain=None, eps=1e-5):
+    """Appends keys k [rows][kv][dh] to sequence 0 from slot 0 on; their codes and scales have to be the exact keys', bit for bit."""
+    c, n = pool.cache, k.shape[0]
+    c.append(None, k, k, pool.ints([0] * n), pool.ints(range(n)), positions=positions and pool.ints([positions]), rope_pairs=pairs,
+             k_norm=gain, rms_eps=eps)
+    pairs = (pool.dh // 2,) if pairs is None else pairs
+    x, g = _np(k), None if gain is None else _np(gain)
+    want = np.array([[op.rope_norm(x[i, h], positions and [positions[i]], pairs, 1e4, g, eps) for h in range(pool.kv)] for i in range(n)])
+    assert np.isfinite(want).all()
+    codes, scales = oq.quantise_heads(want, pool.t)
+    got = pool.bytes()
+    at = [op.place(pool.table, c.k_pages.shape[0], pool.page, 0, j) for j in range(n)]
+    page, off = (np.array(x) for x in zip(*at))
+    assert np.array_equal(got[1].cpu().numpy()[page, :, off], scales)
+    wrong = got[0].cpu().numpy()[page, :, off] != codes
+    assert not wrong.any(), "%d of %d codes, first %s" % (wrong.sum(), wrong.size, np.argwhere(wrong)[0])
+    return want
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("norm", [False, True])
+def test_append_finite_keys_past_the_largest_float(dh, norm):
+    """Rotation, or a gain, carries finite values past what 32 bits hold: they become the largest code, not NaN."""
+    pool = Pool(87, "bf16", 2, dh, 16, [40])
+    big = torch.finfo(torch.bfloat16).max
+    k = torch.tensor(pool.r.choice([-1.0, 1.0], (40, 2, dh)) * pool.r.uniform(0.5, 1, (40, 2, dh)) * big).to(torch.bfloat16)
+    gain = None
+    if norm:
+        k = pool.rows(40, 2)
+        gain = torch.tensor(pool.r.uniform(0.5, 1, dh) * big).to(torch.bfloat16).to(DEV)
+    want = _keys(pool, k.to(DEV), [17 * j for j in range(40)], gain=gain)
+    assert (np.abs(want) > 2.0 ** 128).any()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_append_keys_below_the_smallest_normal_float(dh):
+    """Keys of about 2^-130, which 32 bits hold in steps of 2^-149: one in some tens of thousands is so near to half
+    way between two codes that it would be half way after a rounding to them."""
+    pool = Pool(88, "bf16", 8, dh, 16, [300])
+    gain = torch.tensor(pool.r.uniform(0.5, 1, dh) * 2.0 ** -129).to(torch.bfloat16).to(DEV)
+    want = _keys(pool, pool.rows(300, 8), None, pairs=(), gain=gain)
+    assert np.abs(want).max() < 2.0 ** -126
