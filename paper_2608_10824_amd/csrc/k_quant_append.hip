@@ -179,10 +179,22 @@ __device__ __forceinline__ void append_qk(const PagedAppendArgs& a, const QuantP
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = T::up(x0[s][i]), w[i] = T::up(x1[s][i]);
         if (gain) {
-          Real ss = 0;
+          auto mean_square = [&](Real eps) {
+            Real ss = 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) ss += u[i] * u[i] + w[i] * w[i];
-          const Real r = inverse_root(sum_of_group<GL>(ss) * (Real)(1.f / DH) + (Real)a.eps);
+            for (int i = 0; i < 4; ++i) ss += u[i] * u[i] + w[i] * w[i];
+            return sum_of_group<GL>(ss) * (Real)(1.f / DH) + eps;
+          };
+          Real mean = mean_square(a.eps);
+          // Squares that 32 bits may not hold: of the head times a power of two (the mean is the same in all its lanes).
+          if constexpr (std::is_same<Real, float>::value)
+            if (__builtin_expect(!(mean >= 0x1p-100f && mean <= 0x1p120f), 0)) {
+              const float f = mean > 1.f ? 0x1p-100f : 0x1p100f;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) u[i] *= f, w[i] *= f;
+              mean = mean_square(a.eps * f * f);
+            }
+          const Real r = inverse_root(mean);
 #pragma unroll
           for (int i = 0; i < 4; ++i) u[i] = u[i] * r * T::up(w0[i]), w[i] = w[i] * r * T::up(w1[i]);
         }

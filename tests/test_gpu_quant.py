@@ -1091,3 +1091,16 @@ def test_append_keys_below_the_smallest_normal_float(dh):
     gain = torch.tensor(pool.r.uniform(0.5, 1, dh) * 2.0 ** -129).to(torch.bfloat16).to(DEV)
     want = _keys(pool, pool.rows(300, 8), None, pairs=(), gain=gain)
     assert np.abs(want).max() < 2.0 ** -126
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("eps", [1e-5, 0.0])
+def test_append_norms_whose_squares_leave_32_bits(dh, eps):
+    """Heads of which a square, or the sum of them, is past the largest float, or (without rms_eps) below the smallest."""
+    powers = [0, 40, 62, 63, 64, 65, 100, 125] if eps else [-30, -50, -62, -75, -100, -120]
+
+    def change(q, k, v):
+        for i, p in enumerate(powers):
+            q[i] *= 2.0 ** p
+            k[i] *= 2.0 ** p
+    _append(89, "bf16", 8, 2, dh, 16, [20], [(0, j) for j in range(12)], norm=True, eps=eps, change=change)
