@@ -1104,3 +1104,30 @@ def test_append_norms_whose_squares_leave_32_bits(dh, eps):
             q[i] *= 2.0 ** p
             k[i] *= 2.0 ** p
     _append(89, "bf16", 8, 2, dh, 16, [20], [(0, j) for j in range(12)], norm=True, eps=eps, change=change)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("t", ["bf16", "fp16"])
+def test_append_queries_keep_nan_and_infinities(t, norm):
+    """A query's NaN and infinities come out where the formula has them: in place without a norm, in the partner too
+    where the pair turns, through the whole head with a norm."""
+    heads, dh, n = 3, 128, 6
+    pool = Pool(90, t, 1, dh, 16, [n])
+    q, k = pool.rows(n, heads), pool.rows(n, 1)
+    q[1, 0, 3], q[2, 1, 100], q[3, 2, 5], q[4, 0, 70] = (float(x) for x in ("nan", "nan", "inf", "-inf"))
+    gain = torch.tensor(1 + 0.2 * pool.r.standard_normal(dh)).to(TYPES[t]).to(DEV) if norm else None
+    out = _np(pool.cache.append(q, k, k, pool.ints([0] * n), pool.ints(range(n)), rope_pairs=(32,), q_norm=gain))
+    x, u = _np(q), _u(t)
+    for i in range(n):
+        for h in range(heads):
+            with np.errstate(invalid="ignore"):
+                want = op.rope_norm(x[i, h], [i], (32,), 1e4, None if gain is None else _np(gain), 1e-5)
+            fine = np.isfinite(want)
+            assert np.array_equal(np.isnan(out[i, h]), np.isnan(want)), (i, h)
+            inf = np.isinf(want)
+            assert np.array_equal(out[i, h][inf], want[inf]), (i, h)
+            mag = 2 * np.abs(want[fine]).max(initial=0)   # at least |x| + |y| of any pair
+            with np.errstate(invalid="ignore"):
+                off = np.abs(out[i, h] - want) - u * np.abs(want) - mag * (2.0 ** -20 + 136 * 2.0 ** -24) * (1 + u) - _tiny(t)
+            assert off[fine].max(initial=0) <= 0, (i, h)
+    assert np.isnan(out[1, 0]).any() and np.isnan(out[2, 1]).any()
