@@ -1131,3 +1131,28 @@ def test_append_queries_keep_nan_and_infinities(t, norm):
                 off = np.abs(out[i, h] - want) - u * np.abs(want) - mag * (2.0 ** -20 + 136 * 2.0 ** -24) * (1 + u) - _tiny(t)
             assert off[fine].max(initial=0) <= 0, (i, h)
     assert np.isnan(out[1, 0]).any() and np.isnan(out[2, 1]).any()
+
+
+@pytest.mark.parametrize("t,dh", [("bf16", 64), ("fp16", 64), ("fp16", 128)])
+def test_a_long_append_of_other_types_is_its_parts(t, dh):
+    """As above for the other types and heads, with rows that skip slots and rows of no sequence."""
+    from paper_2608_10824_amd.paged import QuantPagedCache
+    heads, kv, page, n = 32, 8, 64, 26000 if dh == 64 else 13000
+    assert n * (4 * heads + 6 * kv) * dh > 256 << 20 and n // 2 * (4 * heads + 6 * kv) * dh < 256 << 20
+    g = torch.Generator(device=DEV).manual_seed(91)
+    q, k, v = torch.randn(n, heads + 2 * kv, dh, generator=g, device=DEV).to(TYPES[t]).split([heads, kv, kv], dim=1)
+    gain = torch.randn(dh, generator=g, device=DEV).to(TYPES[t])
+    columns = n * 9 // 8 // page + 1
+    caches = [QuantPagedCache.empty(columns, page, kv, dh, 1, columns, dtype=TYPES[t], device=DEV) for _ in range(2)]
+    for c in caches:
+        c.page_table.copy_(torch.randperm(columns, generator=torch.Generator().manual_seed(4))[None])
+    at = torch.arange(n, device=DEV)
+    slot = (at * 9 // 8).int()
+    seq = torch.where(at % 1001 == 1000, -1, 0).int()
+    whole = caches[0].append(q, k, v, seq, slot, q_norm=gain, k_norm=gain)
+    for a, b in ((0, n // 2), (n // 2, n)):
+        part = caches[1].append(q[a:b], k[a:b], v[a:b], seq[a:b], slot[a:b], q_norm=gain, k_norm=gain)
+        assert torch.equal(whole[a:b], part)
+    for name in ("k_pages", "k_scales", "v_pages", "v_scales"):
+        assert torch.equal(*(getattr(c, name).view(torch.uint8) for c in caches)), name
+    assert (caches[0].k_pages.view(torch.uint8) != 0).any() and (caches[0].v_pages.view(torch.uint8) != 0).any()
