@@ -84,11 +84,6 @@ __device__ __forceinline__ int scale_code(float most) {
 // 2^-e of a scale code from 1 to 253.
 __device__ __forceinline__ float inverse_scale(int code) { return __uint_as_float((uint32_t)(254 - code) << 23); }
 
-// Two values, divided by their scale, as codes in the low 16 bits.
-__device__ __forceinline__ uint32_t encoded(float a, float b) {
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-}
-
 // Where a row goes: its page (-1: nowhere) and the slot in it.
 struct QuantPlace {
   int page, off;
