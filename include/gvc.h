@@ -473,13 +473,14 @@ int32_t gvc_paged_check(const gvc_paged_desc* desc, const int32_t* page_table, c
  * have desc.dtype. */
 
 /* Rows into the pages, quantised as they are written: k after norm and rotation
- * (of rope, as in gvc_paged_append; in fp32, with no rounding to 16 bits between),
- * v as it is.  The scale of a head x is 2^e with the least e >= -126 for which
- * max |x| <= 448 * 2^e, and its codes are x / 2^e rounded to nearest even.  Finite
- * values past the largest code that the 16-bit type holds (61440 in fp16, 1.875 *
- * 2^127 in bf16) become that one; NaN and infinities become NaN codes and do not count for
- * the scale.  So rows that were read from a cache keep their values when they are
- * appended without norm and rotation.  q_out gets q with norm and rotation in 16 bits.
+ * (of rope, as in gvc_paged_append; in double, with no rounding between; angles
+ * are off by at most 2^-46 of themselves), v as it is.  The scale of a head x is
+ * 2^e with the least e >= -126 for which max |x| <= 448 * 2^e, and its codes are
+ * x / 2^e rounded to nearest even.  Finite values past the largest code that the
+ * 16-bit type holds (61440 in fp16, 1.875 * 2^127 in bf16) become that one; NaN and
+ * infinities become NaN codes and do not count for the scale.  So rows that were
+ * read from a cache keep their values when they are appended without norm and
+ * rotation.  q_out gets q with norm and rotation, computed in fp32, in 16 bits.
  * Rows, limits and errors as in gvc_paged_append; where two rows of one call name the same
  * slot, the codes of one may be left with the scale of the other. */
 int32_t gvc_quant_append(const gvc_paged_desc* desc, const gvc_paged_rope* rope, const void* q, int64_t q_stride,

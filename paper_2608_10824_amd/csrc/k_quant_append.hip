@@ -3,11 +3,12 @@
 //
 // The scale of a head is 2^e with the least e for which its largest magnitude is
 // at most 448 * 2^e (from the bits of that magnitude), its codes are the values divided by it,
-// which is exact, rounded once.  A key's norm and rotation are computed in double and
-// not rounded before (high_word), so its codes are those of the exact key unless that is within
-// 2^-40 of half way between two codes, where 32 bits would take the other one in one value of two million.  (That
-// takes 1% of a long call of few key-value heads, 9% where every head has one.)  Queries are computed in 32 bits.
-// Angles are taken in full turns and reduced to [-1/2, 1/2].
+// which is exact, rounded once.  A key's norm and rotation are computed in double (rms_eps is its 32 bits) and
+// not rounded before (high_word), so its codes are those of the exact key unless that is nearer to half way between two
+// codes than the computation's error: 2^-44 of the pair that turns, and 2^-46 of it times the angle, from the turns' 64
+// roundings (with bases of 10^4 and more less than 2^-51 times the position).  32 bits would take the other code in one value of
+// two million.  (Double takes 1% of a long call of few key-value heads, 9% where every head has one.)  Queries are
+// computed in 32 bits.  Angles are taken in full turns, in double, and reduced to [-1/2, 1/2].
 //
 // Everything is read and written once, so HBM bounds long calls and launch and
 // load latency short ones.  One launch of append has two kinds of workgroups, as k_paged_append.hip:
@@ -21,7 +22,7 @@
 //
 // Measured (bf16, 128 to a head): append of 21 627 rows of whole prompts, 32 heads on 8, norm and three axes 99 us,
 // 488 MB at 4.9 TB/s, a copy's rate; of 2368 rows of 16 sequences, about every second slot, 32 heads 31 us, 3.1 TB/s
-// (10 us of it bytes of V that stand alone); one row 6.9 us.  Two or four heads of values to a workgroup, kinds of
+// (10 us of it bytes of V that stand alone); one row 4.0 us, 6.1 to 6.4 between two calls of a graph.  Two or four heads of values to a workgroup, kinds of
 // workgroups in turns: 5 to 10% slower.  Read of 41 000 rows of 8 heads, fp16, 64 us, 303 MB at 4.8 TB/s, of every second
 // slot 34 us (stores that stay in the caches 47); of 282 rows of 32 heads 5.1 us.
 #include "gvc_kernels.h"
@@ -33,7 +34,7 @@ namespace gvc {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kRows = 32;      // rows of a workgroup of values, and 7 on both sides that its runs of eight may reach
-constexpr int kReadThreads = 512, kReadRows = 64;   // (32 rows to 256 threads: 41 000 rows 70 us for 66)
+constexpr int kReadThreads = 512, kReadRows = 64;   // (32 rows to 256 threads: 6% slower, 41 000 rows)
 constexpr int kFill = 4096;    // waves of queries and keys that a call's rows are cut into, at least
 
 // What a call reads and writes once: past the caches' least recent lines where the call is larger than
@@ -341,7 +342,7 @@ __device__ __forceinline__ void append_v(const PagedAppendArgs& a, const QuantPa
     }
 }
 
-// (Seven waves to a SIMD: 72 registers for 74, 98.9 us for 100.9, 21 627 rows.)
+// (Seven waves to a SIMD, 72 registers.  With six, of 74, 21 627 rows took 100.9 us for 98.9.)
 template <class T, int DH, bool STREAM>
 __global__ __launch_bounds__(kThreads, 7) void k_quant_append(const PagedAppendArgs a, const QuantPages pages, int v_blocks,
                                                            int slices) {

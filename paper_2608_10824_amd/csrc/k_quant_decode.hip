@@ -13,7 +13,9 @@
 //  * Sixteen bytes of V (dim-major pages) are a dimension's values of sixteen
 //    slots, two operands of O^T += V^T P^T.  Their scales differ from slot to slot: each
 //    pair is converted twice, with either slot's scale, and a half taken of both.
-// So the operands are what the cache's values are in 16 bits, rounded once.
+// So the operands are what the cache's values are in 16 bits, rounded once; probabilities are rounded to 16 bits before the
+// second product, as gvc_paged.h says (relative difference of outputs from 64 bits over the same codes: 0.0017 to 0.0021 in bf16,
+// 0.0002 to 0.0003 in fp16; 32 bits rounded at the end 0.0016 to 0.0017 and 0.0002).
 //
 // Measured (128 to a head, pages not in the caches): one sequence of 282 slots, 32 heads, bf16, 7.4 us; of
 // 200003, 32 heads on 8, 72.8 us and 4.7 for the join, 413 MB at 5.7 TB/s; 64 of 7 to
@@ -21,9 +23,14 @@
 // start and end take 4 to 5 us, which two workgroups of a compute unit do not hide); 40 with a window of 1000,
 // 28 heads on 4, 14.5 us.
 //
-// Two workgroups to a compute unit: the 185 registers of heads of 128 leave room for two, and in the 168 of three
+// Two workgroups to a compute unit: the 187 to 196 registers of heads of 128 leave room for two, and in the 168 of three
 // they spill (200003 slots 98 to 125 us for 78).  Both tiles' operands in flight at once instead
 // of the next ones behind their use, 81 for 78; 2 or 8 waves to a workgroup 85 and 83.
+//
+// Lists of rows come here by the rule of 16-bit pages (paged_few_rows), else to the 128-row tiles.  Both ways over codes, heads of
+// 128, 32 of them: at the rule's 2^22 row-head-slots or below, one sequence of 280 slots and 234 rows 11.1 us for the tiles' 18.5, four of
+// 1000 and 32 rows each 15.5 for 26.8, one of 4000 and 32 rows 19.6 for 26.3; at twice that, one of 1000 and 262 rows 25.2 for 27.3, four of 280
+// and 234 rows 30.0 for 16.3, one of 4000 and 65 rows 29.9 for 27.7; at four times, one of 1000 34.5 for 34.4, one of 4000 50.4 for 34.4.
 #include "gvc_kernels.h"
 #include "gvc_paged_units.h"
 #include "gvc_quant.h"

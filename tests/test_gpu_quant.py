@@ -2,7 +2,7 @@
 QuantPagedCache (and so through the C ABI).
 
 Bounds (none is fitted).  Attention is held to oracle/paged.py over what the
-codes stand for (exact in both 16-bit types), within the bounds that
+codes stand for (rounded once to the 16-bit type), within the bounds that
 tests/test_gpu_paged.py derives for the 16-bit cache: scores, exponentials
 and sums in fp32, each probability rounded once to 16 bits, the output once.
  Values are quantised as they come: codes and scales have to be the oracle's, bit
